@@ -316,6 +316,131 @@ int mtad_debug_set_wait(mtad_ctx* ctx, unsigned int wait_limit, int no_operands)
  * when the process is given fewer SMs later on. */
 int mtad_debug_set_path(mtad_ctx* ctx, int path);
 
+/* ---- Operators around a decoder that the caller runs -------------------------------------------------------------
+ * The calls above verify drafts with a Llama-style forward of the library's own over contiguous caches.  A program whose target is
+ * another decoder, or whose caches are kept in pages, runs that forward itself and takes the steps around it from here: the new rows
+ * enter the cache (mtad_paged_append), attend to it (mtad_paged_attention), drafted tokens are accepted from the
+ * rows of logits (mtad_accept_chain, mtad_accept_chain_spd), and a cache that has grown too long gives up the tokens
+ * that drew the least attention (mtad_paged_evict).  No context: every call is enqueued on `stream` of the current
+ * device and may be captured into a graph; what it needs to keep lies in the caller's arrays.  Calls that run at the same time
+ * must not share a workspace or outputs.  Sizes that are on the device (lengths, row counts, page ids) are checked by
+ * the kernels: a value out of range is never used as an address, it sets a MTAD_ST_* bit in the sequence's status word.
+ *
+ * A cache in pages.  Page p of a layer holds page_size slots of every KV head; sequence b's slot j is slot j % page_size of
+ * page table[b * table_stride + j / page_size].  Element d of (page, head, slot) lies at page * page_stride + head *
+ * head_stride + slot * slot_stride + d of k_pages, and in the same place of v_pages.  All strides count elements and are
+ * multiples of 8, both pointers 16-byte aligned.  One layer of the contiguous cache above is such a cache: page_size =
+ * kv_capacity, table[b] = b.  Sequences may share pages that are only read. */
+enum { MTAD_BF16 = 0, MTAD_F16 = 1, MTAD_F32 = 2 };
+#define MTAD_PAGED_MAX_BATCH 4096       /* sequences per call */
+#define MTAD_PAGED_MAX_HEADS 1024
+#define MTAD_PAGED_MAX_HEAD_DIM 256     /* multiples of 8 */
+#define MTAD_PAGED_MAX_LEN 0x3fffffff   /* slots of a sequence */
+
+typedef struct mtad_paged_kv {
+    void *k_pages, *v_pages;            /* device */
+    const int32_t* table;               /* device [batch][table_stride]: page ids; entries behind a sequence's last page are not read */
+    int64_t page_stride, head_stride, slot_stride, table_stride;
+    int32_t dtype;                      /* MTAD_BF16 or MTAD_F16 */
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+    int32_t max_pages;                  /* entries of a table row */
+} mtad_paged_kv;
+
+/* New rows enter the cache.  Sequence b has n = n_rows[b] rows (rows where n_rows is NULL); row r goes to slot lens[b] - n + r: lens
+ * counts the slots after the call.  With rope_base >= 1 queries and keys are turned by the rotary embedding (half-split pairing (i, i +
+ * head_dim/2), the angle reduced in 64 bits) at position pos[b] + r, or at the slot where pos is NULL; pos differs from the slot once
+ * a cache has been thinned by mtad_paged_evict.  rope_base = 0: no rotation.  The arithmetic is fp32, rounded once to the cache's
+ * type.  Rows beyond n_rows[b] are not read or written.  q_out may be q itself (same type, same strides).  Two rows never share a
+ * slot as long as no two sequences' tables share a page that is written here. */
+typedef struct mtad_paged_rows {
+    const int32_t *lens, *n_rows, *pos; /* device [batch]; n_rows, pos may be NULL */
+    const void *q, *k, *v;              /* device [batch][rows][heads][head_dim] of `dtype`, 16-byte aligned; q NULL with n_q_heads = 0 */
+    void* q_out;                        /* device, the cache's type */
+    uint32_t* status;                   /* device [batch], bits are added: MTAD_ST_KV_OVERFLOW, MTAD_ST_RANGE; may be NULL */
+    int64_t q_stride_seq, q_stride_row, q_stride_head;        /* elements, multiples of 8 (of 4 for fp32) */
+    int64_t kv_stride_seq, kv_stride_row, kv_stride_head;     /* of k and v */
+    int64_t out_stride_seq, out_stride_row, out_stride_head;
+    int32_t dtype;                      /* of q, k, v: the cache's, or MTAD_F32 */
+    int32_t batch, rows, n_q_heads;     /* rows <= MTAD_MAX_NODES + 1 */
+    float rope_base;
+} mtad_paged_rows;
+int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* call, void* stream);
+
+/* Attention of the new rows over the cache: out[b,r,h] = sum_j p_j V[j], p = softmax over the slots j that the row sees
+ * of scale * q[b,r,h] . K[j]; query head h uses KV head h / (n_q_heads / n_kv_heads).  Row r of sequence b stands at slot
+ * at = lens[b] - n + r (n = n_rows[b], or rows) and sees j <= at; with window > 0 only j > at - window or j < sinks.
+ * A row that sees nothing (length 0, or at < 0) gives zeros and lse -inf.  Infinities and NaN in slots that a row does not
+ * see do not reach it.  Rows beyond n_rows[b] are left as they were.  weights, if given, accumulates what mtad_paged_evict
+ * selects by: weights[b][kv head][j] += the sum of p_j over the sequence's rows and the heads of the group, for visible j;
+ * everything else is left alone.  max_len bounds the lengths, and so does what a table row can hold (a longer one is cut to it and flagged MTAD_ST_KV_OVERFLOW, a slot whose
+ * table entry names no page is taken as zeros and flagged MTAD_ST_RANGE) and sizes the launch and the workspace.
+ * Scores, sums and statistics are fp32, the output is rounded once.  Results do not change from call to call.
+ * The workspace (256-byte aligned) holds nothing between calls. */
+typedef struct mtad_paged_attn {
+    const int32_t *lens, *n_rows;       /* device [batch]; n_rows may be NULL */
+    const void* q;                      /* device [batch][rows][n_q_heads][head_dim], the cache's type, 16-byte aligned */
+    void* out;                          /* the same; must not be q */
+    float* lse;                         /* device [batch][rows][n_q_heads] log of the softmax sums, may be NULL */
+    float* weights;                     /* device, may be NULL */
+    uint32_t* status;                   /* device [batch], bits are added; may be NULL */
+    int64_t q_stride_seq, q_stride_row, q_stride_head;        /* elements, multiples of 8 */
+    int64_t out_stride_seq, out_stride_row, out_stride_head;
+    int64_t weights_stride_seq, weights_stride_head;
+    int32_t batch, rows, n_q_heads;     /* rows <= MTAD_MAX_NODES + 1 */
+    int32_t window, sinks;              /* window 0: every slot up to the row's own */
+    int32_t max_len;
+    float scale;                        /* 0: 1 / sqrt(head_dim) */
+} mtad_paged_attn;
+int mtad_paged_attention_workspace(const mtad_paged_kv* kv, const mtad_paged_attn* call, size_t* out_bytes);
+int mtad_paged_attention(const mtad_paged_kv* kv, const mtad_paged_attn* call, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction, per sequence and KV head.  Where lens[b] > keep, the first `first` slots, the last `recent` ones and of the rest those
+ * with the largest scores stay, keep in all (first + recent <= keep; equal scores: the lower slot; NaN counts as larger than
+ * every number).  They move to slots 0 .. keep - 1 in the order of their slots, so that the last tokens stay the last; slots from keep
+ * on are left as they were.  kept[b][h][i] is the former slot of slot i (-1 from the new length on), scores_out[b][h][i] its score;
+ * scores_out may be scores itself for max_len up to 327680 (MTAD_E_UNIMPLEMENTED beyond).  new_lens[b] = min(lens[b], keep); it
+ * must not be lens.  The pages of a sequence that is longer than keep must be its own: no other table row, nor another place
+ * of its own row, may name them.  A length beyond max_len, or beyond what a table row can hold, is cut to it (MTAD_ST_KV_OVERFLOW); a row whose slot or whose new slot has no
+ * page is not moved (MTAD_ST_RANGE). */
+typedef struct mtad_paged_eviction {
+    const int32_t* lens;                /* device [batch] */
+    const float* scores;                /* device [batch][kv head][slot] */
+    int32_t* kept;                      /* device [batch][n_kv_heads][keep] */
+    int32_t* new_lens;                  /* device [batch] */
+    float* scores_out;                  /* device, may be NULL */
+    uint32_t* status;                   /* device [batch], bits are added; may be NULL */
+    int64_t scores_stride_seq, scores_stride_head, out_stride_seq, out_stride_head;
+    int32_t batch, max_len, keep, first, recent;
+} mtad_paged_eviction;
+int mtad_paged_evict(const mtad_paged_kv* kv, const mtad_paged_eviction* call, void* stream);
+
+/* The accept rules on rows of logits.  Row i of sequence b is the target's distribution before drafted token i (row gamma: after
+ * the last), divided by the temperature; any constant may have been added to a row.  n_draft[b] <= gamma drafted tokens count
+ * (NULL: all gamma), the sequence then has n_draft[b] + 1 rows; what lies beyond is not read, its outputs are not written.
+ * mtad_accept_chain is the rule of mtad_verify_chain, mtad_accept_chain_spd that of mtad_verify_chain_spd; draft_rows are the
+ * auxiliary model's rows in the same type.  The last token is drawn with last_uniform [batch][vocab] as the argmax of w_v / -log u_v, w the
+ * target's row, or max(0, p - q) at a rejection (lowest id among equals; tokens with w = 0 never).  Logits of -infinity are
+ * tokens of probability 0; a row that has nothing else, or a NaN or +infinity, flags MTAD_ST_NONFINITE: nothing accepted, n_out =
+ * 0.  Also MTAD_ST_BAD_TOKEN, MTAD_ST_BAD_COUNT.  Outputs as for the verify calls with N = D = gamma (row_cand, row_cand_lp are not
+ * written; node_LP by the first rule only). */
+typedef struct mtad_accept_rows {
+    const void* logits;                 /* device [batch][gamma + 1][vocab] */
+    int64_t logits_stride_seq, logits_stride_row;             /* elements */
+    int64_t draft_stride_seq, draft_stride_row;               /* of draft_rows [batch][gamma][vocab] */
+    const int32_t* draft_tok;           /* device [batch][gamma] */
+    const int32_t* n_draft;             /* device [batch] or NULL */
+    const float* last_uniform;          /* device [batch][vocab] in (0,1) */
+    int32_t dtype;                      /* of the rows: MTAD_BF16, MTAD_F16 or MTAD_F32 */
+    int32_t batch, gamma, vocab;        /* gamma <= MTAD_MAX_DEPTH */
+    float temperature, draft_temperature;                     /* > 0; 1 leaves the rows as they are */
+} mtad_accept_rows;
+int mtad_accept_chain(const mtad_accept_rows* call, const float* draft_logq, float log_tau, const mtad_result* out, void* stream);
+int mtad_accept_chain_spd(const mtad_accept_rows* call, const void* draft_rows, const float* accept_uniform, const mtad_result* out,
+                          void* stream);
+
+/* CUDA error code of this thread's last call of the operators above that returned MTAD_E_CUDA, 0 if its last call succeeded. */
+int mtad_ops_cuda_error(void);
+
 const char* mtad_status_str(int status);
 int mtad_last_cuda_error(const mtad_ctx* ctx);
 

@@ -5,6 +5,8 @@ The product is the C-ABI library built from csrc/ (see include/mtad.h); this pac
 from .binding import (Context, ModelDesc, MtadError, Result, ResultBuffers, load_library, log_tau, make_desc,
                       mtad_workspace_bytes, mtad_kernel_launches, EXPORTS, LIB_PATH,
                       KERNEL_CLASSES)
+from .ops import accept_chain, accept_chain_spd, paged_append, paged_attention, paged_evict
 
 __all__ = ["Context", "ModelDesc", "MtadError", "Result", "ResultBuffers", "load_library", "log_tau", "make_desc",
-           "mtad_workspace_bytes", "mtad_kernel_launches", "EXPORTS", "LIB_PATH", "KERNEL_CLASSES"]
+           "mtad_workspace_bytes", "mtad_kernel_launches", "EXPORTS", "LIB_PATH", "KERNEL_CLASSES",
+           "accept_chain", "accept_chain_spd", "paged_append", "paged_attention", "paged_evict"]

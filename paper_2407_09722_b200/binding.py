@@ -48,7 +48,9 @@ EXPORTS = ("mtad_workspace_bytes", "mtad_create", "mtad_destroy", "mtad_seq_set"
            "mtad_profile_begin", "mtad_profile_end", "mtad_kernel_launches", "mtad_verify_chain_static",
            "mtad_debug_gemm", "mtad_set_warp", "mtad_set_draft_warp", "mtad_profile_grouped",
            "mtad_verify_chain_spd", "mtad_seq_hint", "mtad_debug_set_wait", "mtad_audit_extents",
-           "mtad_debug_check_canaries", "mtad_debug_region", "mtad_debug_set_path")
+           "mtad_debug_check_canaries", "mtad_debug_region", "mtad_debug_set_path", "mtad_paged_append",
+           "mtad_paged_attention_workspace", "mtad_paged_attention", "mtad_paged_evict", "mtad_accept_chain",
+           "mtad_accept_chain_spd", "mtad_ops_cuda_error")
 MTAD_STATIC_SCRATCH_BYTES = 16 << 20
 MTAD_ST_TIMEOUT, MTAD_ST_AUX_PENDING, MTAD_ST_NONFINITE, MTAD_ST_RANGE = 32, 64, 128, 256      # device status bits (mtad.h)
 KERNEL_CLASSES = ("prepare", "norm", "gemm", "rope_append", "attention", "lm_reduce", "accept", "commit")

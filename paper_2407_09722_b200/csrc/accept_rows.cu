@@ -1,0 +1,330 @@
+// The accept rules on rows of logits that the caller's decoder wrote: a draft chain per sequence, the joint-likelihood threshold of
+// Algorithm 1 or the rule of vanilla speculative decoding (Sec. 2.2, steps 2-4).
+//
+// With z the target's rows over a temperature, lp_i = z_i[x_i] - lse(z_i):
+//     threshold    prefix j passes iff sum_{i <= j} lp_i - log q(x_{1:j}) > log tau, the longest passing one is accepted;
+//     speculative  token i is accepted iff log u_i < lp_i - lq_i, up to the first rejection.
+// The last token is a draw from w = p (nothing rejected, or the threshold rule) or w = max(0, p - q) at the rejected position: the
+// argmax of w_v / -log u_v, the same as the argmax of log w_v - log(-log u_v) without two logarithms per token.
+//
+// Every row is read once for its log-sum-exp, one row and the uniforms again for the draw: bound by those bytes, at small
+// batches by latency.  A cluster of eight blocks has a sequence, a block an eighth of the vocabulary; warps take (row, part) tasks, a
+// running maximum and sum a lane; rows' statistics and the draw's candidates cross the cluster in distributed shared memory, so
+// the call is one launch and needs no workspace.  Statistics are fp32, merged in a fixed order.
+#include <cooperative_groups.h>
+#include <math.h>
+#include <math_constants.h>
+
+#include "paged.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace mtad {
+
+namespace {
+
+constexpr int AC_CLUSTER = 8, AC_THREADS = 512, AC_WARPS = AC_THREADS / 32;
+constexpr int AC_ROWS = 2 * MTAD_MAX_DEPTH + 1, AC_PARTS = 8;
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct AcceptRowsArgs {
+    const void *z, *q;               // target rows [B, gamma + 1, V], auxiliary rows [B, gamma, V] or null (threshold rule)
+    long long z_sb, z_sr, q_sb, q_sr;
+    const int32_t *tok, *n_draft;
+    const float *draft_logq, *u_accept, *u_last;
+    float z_mul, q_mul, log_tau;     // 1 / temperature
+    int gamma, V;
+    mtad_result out;
+};
+
+struct Stat {
+    float m, s;                      // sum of exp(x - m)
+};
+__device__ __forceinline__ float ex2a(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ Stat merge(const Stat& a, const Stat& b) {
+    const float m = fmaxf(a.m, b.m);
+    if (m == -CUDART_INF_F) return Stat{m, a.s + b.s};    // (sums of 0, or NaN)
+    return Stat{m, a.s * (a.m == m ? 1.f : ex2a((a.m - m) * LOG2E)) + b.s * (b.m == m ? 1.f : ex2a((b.m - m) * LOG2E))};
+}
+template <int N>
+__device__ __forceinline__ void take(Stat& st, const float (&x)[N]) {
+    float m = st.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+    if (m > st.m) { st.s *= st.m == -CUDART_INF_F ? 0.f : ex2a((st.m - m) * LOG2E); st.m = m; }
+    const float r = m == -CUDART_INF_F ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += ex2a((x[i] - r) * LOG2E);
+    st.s += s;
+}
+
+template <typename T> struct Row;
+template <> struct Row<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void vec(const uint4& w, float (&x)[4]) {
+        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+    }
+    static __device__ __forceinline__ float one(float x) { return x; }
+};
+template <typename T> struct Row16 {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void vec(const uint4& w, float (&x)[8]) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Num<T>::unpack(u[i]);
+            x[2 * i] = f.x; x[2 * i + 1] = f.y;
+        }
+    }
+    static __device__ __forceinline__ float one(T x) { return Num<T>::to(x); }
+};
+template <> struct Row<__nv_bfloat16> : Row16<__nv_bfloat16> {};
+template <> struct Row<__half> : Row16<__half> {};
+
+// Statistics of elements [v0, v1) of a row, times mul, by one warp: 16-byte loads, four in flight a lane; what lies before the
+// first 16-byte boundary and behind the last (rows of odd vocabularies begin anywhere) one by one.
+template <typename T>
+__device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float mul, int lane) {
+    constexpr int N = Row<T>::N, U = 4;
+    Stat st{-CUDART_INF_F, 0.f};
+    const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row + v0) & 15)) & 15) / (int)sizeof(T);
+    const int a0 = min(v0 + skip, v1), nv = (v1 - a0) / N, tail = a0 + nv * N;
+    const uint4* p = reinterpret_cast<const uint4*>(row + a0);
+    for (int i = lane; i < nv; i += 32 * U) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * 32 < nv) w[u] = __ldg(p + i + u * 32);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * 32 < nv) {
+                float x[N];
+                Row<T>::vec(w[u], x);
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] *= mul;
+                take<N>(st, x);
+            }
+    }
+    for (int v = v0 + lane; v < a0; v += 32) { const float x[1] = {Row<T>::one(row[v]) * mul}; take<1>(st, x); }
+    for (int v = tail + lane; v < v1; v += 32) { const float x[1] = {Row<T>::one(row[v]) * mul}; take<1>(st, x); }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) st = merge(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o)});
+    return st;
+}
+
+struct Best {                        // best candidate of the draw, and of a draw from p alone
+    float y, y2;
+    int v, v2;
+};
+__device__ __forceinline__ void better(Best& a, float y, int v, float y2, int v2) {
+    if (y > a.y || (y == a.y && v < a.v)) { a.y = y; a.v = v; }
+    if (y2 > a.y2 || (y2 == a.y2 && v2 < a.v2)) { a.y2 = y2; a.v2 = v2; }
+}
+
+template <typename T>
+__global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(AC_THREADS, 2) accept_rows_kernel(const AcceptRowsArgs a) {
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), b = blockIdx.x / AC_CLUSTER, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ Stat s_part[AC_ROWS * AC_PARTS];
+    __shared__ Stat s_row[AC_ROWS];                       // read by the cluster
+    __shared__ Best s_best[AC_WARPS], s_block;            // s_block: read by the cluster
+    __shared__ float s_lse[AC_ROWS];
+    __shared__ int s_eta;
+    const int D = a.gamma, V = a.V;
+    const int given = a.n_draft ? __ldg(a.n_draft + b) : D, g = min(max(given, 0), D);
+    const bool spd = a.q != nullptr;
+    const int rows = g + 1 + (spd ? g : 0);
+    const T* z = static_cast<const T*>(a.z) + (long long)b * a.z_sb;
+    const T* q = spd ? static_cast<const T*>(a.q) + (long long)b * a.q_sb : nullptr;
+    const int per = ((V + AC_CLUSTER - 1) / AC_CLUSTER + 7) / 8 * 8, v0 = min(rank * per, V), v1 = min(v0 + per, V);
+    // tokens and their logits, early: a lane per drafted token
+    uint32_t bits = given == g ? 0u : MTAD_ST_BAD_COUNT;
+    int x = 0;
+    float zx = 0.f, qx = 0.f;
+    if (warp == 0) {
+        bool bad = false;
+        if (lane < g) {
+            x = __ldg(a.tok + (long long)b * D + lane);
+            bad = (unsigned)x >= (unsigned)V;
+            if (!bad) {
+                zx = Row<T>::one(z[(long long)lane * a.z_sr + x]) * a.z_mul;
+                if (spd) qx = Row<T>::one(q[(long long)lane * a.q_sr + x]) * a.q_mul;
+            }
+        }
+        if (__any_sync(0xffffffffu, bad)) bits |= MTAD_ST_BAD_TOKEN;
+    }
+    // ---- log-sum-exp of every row
+    const int parts = min(AC_PARTS, max(1, (v1 - v0) / (Row<T>::N * 128))), step = (v1 - v0 + parts - 1) / parts;
+    for (int t = warp; t < rows * parts; t += AC_WARPS) {
+        const int r = t / parts, p = t - r * parts, e0 = min(v0 + p * step, v1), e1 = min(e0 + step, v1);
+        const Stat st = r <= g ? row_stat<T>(z + (long long)r * a.z_sr, e0, e1, a.z_mul, lane)
+                               : row_stat<T>(q + (long long)(r - g - 1) * a.q_sr, e0, e1, a.q_mul, lane);
+        if (lane == 0) s_part[t] = st;
+    }
+    __syncthreads();
+    if (tid < rows) {
+        Stat st = s_part[tid * parts];
+        for (int p = 1; p < parts; ++p) st = merge(st, s_part[tid * parts + p]);
+        s_row[tid] = st;
+    }
+    cluster.sync();
+    if (tid < rows) {
+        Stat st = *cluster.map_shared_rank(&s_row[tid], 0);
+        for (int k = 1; k < AC_CLUSTER; ++k) st = merge(st, *cluster.map_shared_rank(&s_row[tid], k));
+        s_lse[tid] = st.m + logf(st.s);
+    }
+    __syncthreads();
+    // ---- the accepted prefix (warp 0 of every block; the first block writes)
+    if (warp == 0) {
+        const bool w = rank == 0;
+        bool finite = true;
+        for (int r = lane; r < rows; r += 32) finite = finite && isfinite(s_lse[r]);
+        if (!__all_sync(0xffffffffu, finite)) bits |= MTAD_ST_NONFINITE;
+        const float lp = lane < g ? zx - s_lse[lane] : 0.f;
+        int eta = 0;
+        float gap = CUDART_INF_F, LP = lp;
+        if (spd) {
+            const float ratio = lane < g ? fminf(0.f, lp - (qx - s_lse[g + 1 + lane])) : 0.f;   // (NaN, 0 over 0: rejected, below)
+            const float lu = lane < g ? logf(__ldg(a.u_accept + (long long)b * D + lane)) : 0.f;
+            const bool ok = lane < g && lp > -CUDART_INF_F && lu < ratio;
+            const uint32_t no = __ballot_sync(0xffffffffu, !ok);
+            eta = min(no ? __ffs(no) - 1 : 32, g);
+            if (lane <= eta && lane < g) gap = fabsf(lu - ratio);
+        } else {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float y = __shfl_up_sync(0xffffffffu, LP, o);
+                if (lane >= o) LP += y;
+            }
+            const float over = lane < g ? LP - __ldg(a.draft_logq + (long long)b * D + lane) : 0.f;
+            // (log_tau = -inf: every prefix passes)
+            const bool ok = lane < g && (a.log_tau == -CUDART_INF_F || over > a.log_tau);
+            const uint32_t yes = __ballot_sync(0xffffffffu, ok);
+            eta = yes ? 32 - __clz(yes) : 0;
+            if (lane < g) gap = fabsf(over - a.log_tau);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) gap = fminf(gap, __shfl_xor_sync(0xffffffffu, gap, o));
+        if (lane == 0) s_eta = bits ? -1 : eta;
+        if (w) {
+            const mtad_result& o = a.out;
+            if (bits) eta = 0;
+            if (lane == 0) {
+                o.status[b] = bits;
+                o.eta[b] = eta;
+                o.winner[b] = eta - 1;
+                o.n_out[b] = bits ? 0 : eta + 1;
+                if (o.margin && !bits) { o.margin[b * 2] = gap; o.margin[b * 2 + 1] = CUDART_INF_F; }
+            }
+            if (!bits) {
+                if (lane < eta) {
+                    o.path[(long long)b * D + lane] = lane;
+                    o.out_tok[(long long)b * (D + 1) + lane] = x;
+                    o.out_lp[(long long)b * (D + 1) + lane] = lp;
+                }
+                if (lane < g && o.node_lp) o.node_lp[(long long)b * D + lane] = lp;
+                if (lane < g && o.node_LP && !spd) o.node_LP[(long long)b * D + lane] = LP;
+                if (o.row_lse) for (int r = lane; r <= g; r += 32) o.row_lse[(long long)b * (D + 1) + r] = s_lse[r];
+            }
+        }
+    }
+    __syncthreads();
+    const int eta = s_eta;
+    // ---- the last token: this block's share of the vocabulary
+    Best best{-CUDART_INF_F, -CUDART_INF_F, 0x7fffffff, 0x7fffffff};
+    if (eta >= 0) {                                       // (the same in every block of the cluster)
+        const T* row = z + (long long)eta * a.z_sr;
+        const bool rest = spd && eta < g;
+        const T* qrow = rest ? q + (long long)eta * a.q_sr : row;
+        const float lse = s_lse[eta], lse_q = rest ? s_lse[g + 1 + eta] : 0.f;
+        const float* u = a.u_last + (long long)b * V;
+#pragma unroll 4
+        for (int v = v0 + tid; v < v1; v += AC_THREADS) {
+            const float p = ex2a((Row<T>::one(row[v]) * a.z_mul - lse) * LOG2E);
+            const float e = -logf(__ldg(u + v));
+            float w = p;
+            if (rest) w = fmaxf(p - ex2a((Row<T>::one(qrow[v]) * a.q_mul - lse_q) * LOG2E), 0.f);
+            // (a weight of zero is no candidate)
+            better(best, w > 0.f ? w / e : -CUDART_INF_F, w > 0.f ? v : 0x7fffffff, p > 0.f ? p / e : -CUDART_INF_F, p > 0.f ? v : 0x7fffffff);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const float y = __shfl_xor_sync(0xffffffffu, best.y, o), y2 = __shfl_xor_sync(0xffffffffu, best.y2, o);
+            const int v = __shfl_xor_sync(0xffffffffu, best.v, o), v2 = __shfl_xor_sync(0xffffffffu, best.v2, o);
+            better(best, y, v, y2, v2);
+        }
+    }
+    if (lane == 0) s_best[warp] = best;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < AC_WARPS; ++w) better(best, s_best[w].y, s_best[w].v, s_best[w].y2, s_best[w].v2);
+        s_block = best;
+    }
+    cluster.sync();
+    if (rank == 0 && tid == 0 && eta >= 0) {
+        for (int k = 1; k < AC_CLUSTER; ++k) {
+            const Best c = *cluster.map_shared_rank(&s_block, k);
+            better(best, c.y, c.v, c.y2, c.v2);
+        }
+        // (no mass left where p and q agree to the last bit: a draw from p)
+        const int t = best.v != 0x7fffffff ? best.v : best.v2 != 0x7fffffff ? best.v2 : 0;
+        a.out.out_tok[(long long)b * (D + 1) + eta] = t;
+        a.out.out_lp[(long long)b * (D + 1) + eta] = Row<T>::one(z[(long long)eta * a.z_sr + t]) * a.z_mul - s_lse[eta];
+    }
+    cluster.sync();                                       // (no block leaves while the first reads its candidates)
+}
+
+int accept_rows(const mtad_accept_rows* c, const float* draft_logq, float log_tau, const void* q, const float* u_accept,
+                const mtad_result* out, void* stream) {
+    if (!c || !out || !c->logits || !c->last_uniform || c->batch < 1 || c->gamma < 0 || c->vocab < 1) return MTAD_E_INVALID;
+    if (c->gamma > 0 && (!c->draft_tok || !out->path)) return MTAD_E_INVALID;
+    if (!out->eta || !out->winner || !out->n_out || !out->out_tok || !out->out_lp || !out->status) return MTAD_E_INVALID;
+    if (c->dtype != MTAD_BF16 && c->dtype != MTAD_F16 && c->dtype != MTAD_F32) return MTAD_E_INVALID;
+    if (c->batch > MTAD_PAGED_MAX_BATCH || c->gamma > MTAD_MAX_DEPTH) return MTAD_E_CAPACITY;
+    if (!(c->temperature > 0.f) || !isfinite(c->temperature)) return MTAD_E_INVALID;
+    if (c->logits_stride_seq < 0 || c->logits_stride_row < 0 || (q && (c->draft_stride_seq < 0 || c->draft_stride_row < 0))) return MTAD_E_INVALID;
+    const uintptr_t el = c->dtype == MTAD_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(c->logits) | reinterpret_cast<uintptr_t>(q)) & (el - 1)) return MTAD_E_INVALID;
+    AcceptRowsArgs a{};
+    a.z = c->logits; a.q = q;
+    a.z_sb = c->logits_stride_seq; a.z_sr = c->logits_stride_row; a.q_sb = c->draft_stride_seq; a.q_sr = c->draft_stride_row;
+    a.tok = c->draft_tok; a.n_draft = c->n_draft;
+    a.draft_logq = draft_logq; a.u_accept = u_accept; a.u_last = c->last_uniform;
+    a.z_mul = 1.f / c->temperature; a.q_mul = q ? 1.f / c->draft_temperature : 1.f; a.log_tau = log_tau;
+    a.gamma = c->gamma; a.V = c->vocab;
+    a.out = *out;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const dim3 grid(c->batch * AC_CLUSTER);
+    if (c->dtype == MTAD_F32) accept_rows_kernel<float><<<grid, AC_THREADS, 0, st>>>(a);
+    else if (c->dtype == MTAD_BF16) accept_rows_kernel<__nv_bfloat16><<<grid, AC_THREADS, 0, st>>>(a);
+    else accept_rows_kernel<__half><<<grid, AC_THREADS, 0, st>>>(a);
+    mtad_ops_count(1);
+    return ops_status(cudaGetLastError());
+}
+
+}  // namespace
+
+}  // namespace mtad
+
+using namespace mtad;
+
+extern "C" {
+
+int mtad_accept_chain(const mtad_accept_rows* call, const float* draft_logq, float log_tau, const mtad_result* out, void* stream) {
+    if (!call || (call->gamma > 0 && !draft_logq) || isnan(log_tau) || !(log_tau < 0.f)) return MTAD_E_INVALID;
+    return accept_rows(call, draft_logq, log_tau, nullptr, nullptr, out, stream);
+}
+
+int mtad_accept_chain_spd(const mtad_accept_rows* call, const void* draft_rows, const float* accept_uniform, const mtad_result* out,
+                          void* stream) {
+    if (!call || !draft_rows || !accept_uniform || call->gamma < 1) return MTAD_E_INVALID;
+    if (!(call->draft_temperature > 0.f) || !isfinite(call->draft_temperature)) return MTAD_E_INVALID;
+    return accept_rows(call, nullptr, 0.f, draft_rows, accept_uniform, out, stream);
+}
+
+}  // extern "C"
