@@ -17,12 +17,15 @@
 //  - page ids and offsets are looked up one tile ahead, a lane per key, and handed around by shuffles.
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as two terms of the cache's type
 // (p and what its rounding left), so the 2^-9 of a bf16 probability does not reach the output; the output is rounded once.
+#include <cooperative_groups.h>
 #include <math_constants.h>
 
 #include <algorithm>
 #include <type_traits>
 
 #include "paged.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace mtad {
 
@@ -31,7 +34,8 @@ namespace {
 constexpr int TK = 64;               // keys of a tile
 constexpr int NT = 128;              // threads of a block
 constexpr int MAX_ROWS_BLOCK = 64;   // query rows (rows x heads of the group) of a block
-constexpr int WHOLE_TILES = 4;       // up to so many tiles a head, a block takes a head as a whole and nothing is joined
+constexpr int MAX_CLUSTER = 8;
+constexpr int CLUSTER_TILES = 12;    // tiles of a block up to which a cluster has a head
 
 struct AttnArgs {
     PagedView kv;
@@ -42,10 +46,11 @@ struct AttnArgs {
     float* lse;                      // [B, R, Hq] or null
     long long q_sb, q_sr, q_sh, o_sb, o_sr, o_sh;
     uint32_t* status;
-    int B, R, G, RB, rows_block;     // heads of a group, row blocks, query rows of a block (16 * MT)
+    int B, R, G, RB, rows_block;     // heads of a group, row blocks, query rows of a block
     int window, sinks, max_len;
     float scale2;                    // scale * log2(e)
-    int whole;                       // a block per (sequence, KV head, row block)
+    int even;                        // 16 neighbouring slots, the first a multiple of 16, lie in one page
+    int cluster;                     // blocks of a head; 0: the list is cut evenly over the grid
     int grid;
     // workspace
     long long* plan;                 // [0] tiles of a block, [1 .. B + 1] first tile of every sequence
@@ -63,18 +68,19 @@ struct AttnArgs {
 struct Seq {
     int len, nb, nt, ns, skip;       // tile t of the list is tile t of the cache for t < ns, t + skip beyond
 };
+template <int UNIT>
 __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int b) {
     Seq s;
     const int len = __ldg(a.lens + b);
     s.len = min(max(len, 0), a.max_len);
     s.nb = a.n_rows ? min(max(__ldg(a.n_rows + b), 0), a.R) : a.R;
-    const int total = (s.len + TK - 1) / TK;
+    const int total = (s.len + UNIT - 1) / UNIT;
     s.ns = total;
     s.skip = 0;
     if (a.window > 0) {
         const int first = max(s.len - s.nb - a.window + 1, 0);          // of the first row
-        const int ns = (min(a.sinks, s.len) + TK - 1) / TK;
-        const int from = max(first / TK, ns);
+        const int ns = (min(a.sinks, s.len) + UNIT - 1) / UNIT;
+        const int from = max(first / UNIT, ns);
         if (from < total) { s.ns = ns; s.skip = from - ns; }
     }
     // (a sequence without a visible slot still has a tile: its rows are written)
@@ -86,6 +92,7 @@ struct Cursor {                      // a tile of the list
     int b, hr, t;                    // sequence, KV head * row blocks + row block, tile
     Seq s;
 };
+template <int UNIT>
 __device__ __forceinline__ void advance(const AttnArgs& a, Cursor& c) {
     if (++c.t < c.s.nt) return;
     c.t = 0;
@@ -93,7 +100,7 @@ __device__ __forceinline__ void advance(const AttnArgs& a, Cursor& c) {
     c.hr = 0;
     do {
         if (++c.b >= a.B) return;
-        c.s = seq_of(a, c.b);
+        c.s = seq_of<UNIT>(a, c.b);
     } while (c.s.nt == 0);
 }
 
@@ -110,6 +117,11 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {             // of an 8 x 8 block of 16-bit elements
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 template <typename T>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (std::is_same<T, __half>::value)
@@ -119,203 +131,328 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+constexpr float LN2 = 0.6931471805599453f;
+// of a row's sum: 0 for a row that sees nothing (its output is zero), NaN stays NaN
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
-template <int HD> struct Tile {
+// Byte offset of 16-byte piece c of row r of a tile: the pieces of eight neighbouring rows fall into different banks.  Tiles begin at
+// multiples of 512 bytes, so that the pieces 2 k, 2 k + 1 of a row lie at (address of the pieces 0, 1) ^ (k << 5).
+template <int HD> __device__ __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * HD * 2 + ((c ^ (r & 7)) << 4)); }
+
+template <int HD, int ROWS> struct Tile {
     static constexpr int CH = HD / 8;                    // 16-byte pieces of a row
     static constexpr int BYTES = TK * HD * 2;            // keys (or values) of a tile
-    static constexpr int STAGES = HD == 64 ? 6 : 3;      // 96 KB (192 of heads of 256) on their way or in use
-    static constexpr int BLOCKS = HD == 256 ? 1 : 2;     // blocks of an SM
-    // byte offset of piece c of row r: pieces of eight neighbouring rows fall into different banks
-    static __device__ __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * HD * 2 + ((c ^ (r & 7)) << 4)); }
+    // two blocks on an SM (one with heads of 256): 70 to 105 KB of a block's shared memory on their way or in use
+    static constexpr int STAGES = HD == 64 ? (ROWS <= 16 ? 6 : 4) : (ROWS <= 16 ? 3 : 2);
+    static constexpr int BLOCKS = HD == 256 ? 1 : 2;
+    static constexpr int MT = ROWS <= 16 ? 1 : ROWS / 16;                // warps over the rows; 4 / MT over the keys of a tile
+    static constexpr int Q = ROWS <= 16 ? 0 : ROWS * HD * 2;
+    static constexpr int COLS = MT;                      // parts of the columns in which the warps of a block add their outputs
+    static constexpr int LDO = HD + 4, LDC = HD / COLS + 4;
+    static constexpr int OBUF = ROWS * LDC * 4;
+    static constexpr int SMEM = STAGES * 2 * BYTES + Q;  // and OBUF, for blocks of the list
+    static_assert((4 / MT) * ROWS * LDO * 4 <= STAGES * 2 * BYTES, "the outputs of all warps fit the stages");
 };
-template <int HD, int MT> constexpr int attn_smem() {
-    return Tile<HD>::STAGES * 2 * Tile<HD>::BYTES + MT * 16 * HD * 2 + (MT < 4 ? 16 * HD * 4 : 0);
+
+__device__ __forceinline__ bool sees(const AttnArgs& a, int j, int pos) {
+    return j <= pos && (a.window <= 0 || j > pos - a.window || j < a.sinks);
 }
 
-// T: the cache's type; HD: head_dim rounded up to 64, 128 or 256; MT: 16-row tiles of query rows (the four warps stand MT
-// over the rows by 4 / MT over the keys of a tile)
-template <typename T, int HD, int MT>
-__global__ void __launch_bounds__(NT, Tile<HD>::BLOCKS) attn_kernel(const AttnArgs a) {
-    using L = Tile<HD>;
-    constexpr int KW = 4 / MT, WK = TK / KW, S = L::STAGES, CH = L::CH, PASS = 32 / CH > 0 ? 32 / CH : 1, RW = 16;
-    extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float s_m[4][16], s_l[4][16];
-    __shared__ long long s_scan[4];
-    __shared__ long long s_first[3];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % MT, wk = warp / MT;
-    const int g = lane >> 2, t2 = (lane & 3) * 2;
-    const uint32_t sm = (uint32_t)__cvta_generic_to_shared(smem);
-    const uint32_t sm_q = sm + S * 2 * L::BYTES;
-    float* const obuf = reinterpret_cast<float*>(smem + S * 2 * L::BYTES + MT * 16 * HD * 2);
-    const int HR = a.kv.Hkv * a.RB, chunks = a.kv.hd >> 3;
+// A tile as the cores see it
+struct TileAt {
+    uint32_t k, v;                   // shared memory (Narrow: of the warp's own 16 rows)
+    int j0, first_pos, last_pos;     // slot of the first row there; positions of the sequence's first and last row
+    bool inner, many;                // every slot is visible to every row; the sequence has several rows
+};
+// a slot that some rows of the sequence see and others do not
+__device__ __forceinline__ bool mixed(const AttnArgs& a, const TileAt& t, int j) {
+    return j <= t.last_pos && !(sees(a, j, t.first_pos) && sees(a, j, t.last_pos));
+}
+// whether one of the 16 value rows at `first` that only some rows see holds an infinity or a NaN (per lane)
+template <typename T, int HD>
+__device__ __forceinline__ bool odd_value(const AttnArgs& a, const TileAt& t, int first, int chunks, int lane) {
+    bool odd = false;
+    if (lane < 16 && mixed(a, t, t.j0 + first + lane))
+        for (int c = 0; c < chunks; ++c) {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "r"(t.v + at<HD>(first + lane, c)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = odd || (w[e] & Num<T>::kExp) == Num<T>::kExp || ((w[e] >> 16) & Num<T>::kExp) == Num<T>::kExp;
+        }
+    return odd;
+}
+template <int HD>
+__device__ __forceinline__ void zero_mixed(const AttnArgs& a, const TileAt& t, int first, int lane) {
+    for (int r = 0; r < 16; ++r)
+        if (mixed(a, t, t.j0 + first + r))
+            for (int c = lane; c < HD / 8; c += 32)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(t.v + at<HD>(first + r, c)), "r"(0u) : "memory");
+}
 
-    pdl_trigger();
-    // ---- this block's share of the list
-    long long start, end, per = 0;
-    Cursor P;
-    if (a.whole) {
-        P.b = blockIdx.x / HR;
-        P.hr = blockIdx.x - P.b * HR;
-        P.t = 0;
-        P.s = seq_of(a, P.b);
-        start = 0;
-        end = P.s.nt;
-        if (end == 0) return;
-    } else {
-        const int each = (a.B + NT - 1) / NT, b0 = tid * each, b1 = min(a.B, b0 + each);
-        long long mine = 0;
-        for (int b = b0; b < b1; ++b) mine += (long long)seq_of(a, b).nt * HR;
-        long long incl = mine;
+// The reference of a row's exponentials is raised only when a score passes it by 2^RAISE: sums and outputs stay far inside fp32's range,
+// and most tiles need neither a maximum over lanes nor a rescaling.
+constexpr float RAISE = 6.f;
+
+// Up to 16 query rows: keys stand on the M side of the products, S^T = K Q^T (16 keys x 8 rows a step) and O^T = V^T P^T (16 columns x 8
+// rows), so that eight rows - one token with a group of eight heads, a chain of seven - fill a tile that would be half empty with
+// the queries on that side: half the tensor instructions and half the accumulators.  Every warp has 16 keys of a tile to itself.
+template <typename T, int HD, int ROWS> struct Narrow {
+    using L = Tile<HD, ROWS>;
+    static constexpr int N8 = ROWS / 8, KW = 4;
+    float o[HD / 16][N8][4];         // (column g | g + 8, row 2t | 2t + 1)
+    float m[N8][2], l[N8][2];        // reference (log2 domain) and sum (of this thread's keys) of rows 2t, 2t + 1
+    uint32_t q[HD / 16][N8][2];
+    int pos[N8][2];                  // last visible slot, -1: no such row
+    int g, t2, warp, lane;
+
+    __device__ __forceinline__ void init(int tid) { lane = tid & 31; warp = tid >> 5; g = lane >> 2; t2 = (lane & 3) * 2; }
+    __device__ __forceinline__ void reset() {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += x;
-        }
-        if (lane == 31) s_scan[warp] = incl;
-        __syncthreads();
-        long long before = 0, total = 0;
+        for (int n = 0; n < N8; ++n) {
+            m[n][0] = m[n][1] = -CUDART_INF_F;
+            l[n][0] = l[n][1] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < warp) before += s_scan[w];
-            total += s_scan[w];
+            for (int d = 0; d < HD / 16; ++d) o[d][n][0] = o[d][n][1] = o[d][n][2] = o[d][n][3] = 0.f;
         }
-        per = (total + a.grid - 1) / a.grid;
-        start = per * blockIdx.x;
-        end = min(total, start + per);
-        long long base = before + incl - mine;
-        if (blockIdx.x == 0) {                           // for the second kernel
-            if (tid == 0) { a.plan[0] = per; a.plan[a.B + 1] = total; }
-            long long x = base;
-            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += (long long)seq_of(a, b).nt * HR; }
+    }
+    __device__ __forceinline__ void read_q(const AttnArgs& a, const uint16_t* base, int h, int m0, int rows) {
+#pragma unroll
+        for (int n = 0; n < N8; ++n) {
+            const int row = n * 8 + g, r = (m0 + row) / a.G, hq = h * a.G + (m0 + row) - r * a.G;
+            const uint16_t* src = base + (long long)r * a.q_sr + (long long)hq * a.q_sh + t2;
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int c = k * 16 + e * 8;
+                    q[k][n][e] = row < rows && c < a.kv.hd ? __ldg(reinterpret_cast<const uint32_t*>(src + c)) : 0u;
+                }
         }
-        if (start >= end) return;
-        if (start >= base && start < base + mine) {
-            int b = b0;
-            for (;; ++b) {
-                const long long n = (long long)seq_of(a, b).nt * HR;
-                if (start < base + n) break;
-                base += n;
+    }
+    __device__ __forceinline__ void put_q(const AttnArgs& a, uint32_t, int first_pos, int m0, int rows) {
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = n * 8 + t2 + e;
+                pos[n][e] = row < rows ? first_pos + (m0 + row) / a.G : -1;
             }
-            s_first[0] = b;
-            s_first[1] = start - base;
-        }
-        __syncthreads();
-        P.b = (int)s_first[0];
-        P.s = seq_of(a, P.b);
-        const long long in = s_first[1];
-        P.hr = (int)(in / P.s.nt);
-        P.t = (int)(in - (long long)P.hr * P.s.nt);
     }
-    const int count = (int)(end - start);
-    if (tid == 0 && a.status) {
-        const int len = __ldg(a.lens + P.b);
-        if (len < 0 || len > a.max_len) atomicOr(a.status + P.b, MTAD_ST_KV_OVERFLOW);
-    }
-    Cursor C = P;
-
-    // ---- copies: a warp brings rows 16 * warp .. + 15 of a tile (with MT = 1 the rows that it multiplies)
-    // offset of the row of this lane (lanes 0 .. 15) in the next tile to be copied, -1: nothing there (zeros instead)
-    auto look_up = [&](const Cursor& c) -> long long {
-        const int slot = (c.t < c.s.ns ? c.t : c.t + c.s.skip) * TK + warp * RW + (lane & 15);
-        const int hi = c.s.len - 1, lo = c.s.len - c.s.nb - a.window;     // the slots that some row sees
-        if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return -1;
-        const long long off = slot_offset(a.kv, a.kv.table + (long long)c.b * a.kv.table_stride, slot);
-        if (off < 0 && a.status) atomicOr(a.status + c.b, MTAD_ST_RANGE);
-        return off < 0 ? off : off + (long long)(c.hr / a.RB) * a.kv.head_stride;
-    };
-    auto copy = [&](long long off, int stage) {
-        const uint32_t dk = sm + stage * 2 * L::BYTES, dv = dk + L::BYTES;
-        if constexpr (CH <= 32) {
+    __device__ __forceinline__ void tile(const AttnArgs& a, const TileAt& t, uint32_t, float* scores, int chunks) {
+        float s[N8][4];              // (key g | g + 8, row 2t | 2t + 1)
 #pragma unroll
-            for (int p = 0; p < RW / PASS; ++p) {
-                const int rr = p * PASS + lane / CH, c = lane % CH, r = warp * RW + rr;
-                const long long o = __shfl_sync(0xffffffffu, off, rr);
-                const bool there = o >= 0 && c < chunks;
-                const long long e = there ? o + c * 8 : 0;
-                cp16(dk + L::at(r, c), a.kv.k + e, there);
-                cp16(dv + L::at(r, c), a.kv.v + e, there);
+        for (int n = 0; n < N8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        const uint32_t at_k = t.k + at<HD>(lane & 15, lane >> 4);
+        const uint32_t at_v = t.v + at<HD>((lane >> 4) * 8 + (lane & 7), (lane >> 3) & 1);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+            uint32_t ka[4];
+            ldsm4(ka, at_k ^ (k << 5));
+#pragma unroll
+            for (int n = 0; n < N8; ++n) mma<T>(s[n], ka, q[k][n][0], q[k][n][1]);
+        }
+        bool over = false;
+#pragma unroll
+        for (int n = 0; n < N8; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] *= a.scale2;
+                if (!t.inner && !sees(a, t.j0 + g + (e >> 1) * 8, pos[n][e & 1])) s[n][e] = -CUDART_INF_F;
+                over = over || s[n][e] > m[n][e & 1] + RAISE;
+            }
+            if (scores) {
+                float* z = scores + (n * 8 + t2) * a.score_ld + t.j0 + g;
+                if (pos[n][0] >= 0) { z[0] = s[n][0]; z[8] = s[n][2]; }
+                if (pos[n][1] >= 0) { z[a.score_ld] = s[n][1]; z[a.score_ld + 8] = s[n][3]; }
             }
         }
-    };
-    int ahead = 0;                                        // tiles handed to the copies
-    long long off = look_up(P);
+        if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        if (ahead < count) {
-            copy(off, s);
-            if (++ahead < count) { advance(a, P); off = look_up(P); }
+            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(s[n][e], s[n][e + 2]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+                    const float to = fmaxf(m[n][e], x), f = m[n][e] == to ? 1.f : ex2(m[n][e] - to);
+                    m[n][e] = to;
+                    l[n][e] *= f;
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) { o[d][n][e] *= f; o[d][n][e + 2] *= f; }
+                }
         }
-        cp_commit();
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] = ex2(s[n][e] - (m[n][e & 1] == -CUDART_INF_F ? 0.f : m[n][e & 1]));
+                l[n][e & 1] += s[n][e];
+            }
+        // values that only some rows see: an infinity or NaN among them must not reach the others as 0 * inf.  Such a value row
+        // is added to the rows that see it by hand and zeroed for the product.
+        if (!t.inner && t.many && __any_sync(0xffffffffu, odd_value<T, HD>(a, t, 0, chunks, lane))) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll 1
+                for (int kk = 0; kk < 8; ++kk) {
+                    const int r = half * 8 + kk, j = t.j0 + r;
+                    if (!mixed(a, t, j)) continue;
+#pragma unroll
+                    for (int n = 0; n < N8; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float pr = __shfl_sync(0xffffffffu, s[n][half * 2 + e], (kk << 2) | (lane & 3));
+                            if (sees(a, j, pos[n][e]))
+#pragma unroll
+                                for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+                                    for (int up = 0; up < 2; ++up) {
+                                        uint16_t w;
+                                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(t.v + at<HD>(r, d * 2 + up) + g * 2));
+                                        o[d][n][e + 2 * up] += pr * Num<T>::unpack(w).x;
+                                    }
+                        }
+                }
+            __syncwarp();
+            zero_mixed<HD>(a, t, 0, lane);
+            __syncwarp();
+        }
+        // P^T as the products' second operand: two neighbouring rows of a key are packed and the 8 x 8 blocks transposed
+        uint32_t ph[N8][2], pl[N8][2];
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const float u = s[n][half * 2], v = s[n][half * 2 + 1];
+                const uint32_t hi = Num<T>::pack(u, v);
+                const float2 x = Num<T>::unpack(hi);
+                ph[n][half] = transposed(hi);
+                pl[n][half] = transposed(Num<T>::pack(u - x.x, v - x.y));
+            }
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) {
+            uint32_t va[4];
+            ldsm4t(va, at_v ^ (d << 5));
+#pragma unroll
+            for (int n = 0; n < N8; ++n) {
+                mma<T>(o[d][n], va, ph[n][0], ph[n][1]);
+                mma<T>(o[d][n], va, pl[n][0], pl[n][1]);
+            }
+        }
     }
+    // The rows' statistics over the block's warps to s_ml; o is brought to the block's reference.
+    __device__ __forceinline__ void join_warps(float2* s_part, float2* s_ml) {
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+                if (g == 0) s_part[warp * ROWS + n * 8 + t2 + e] = make_float2(m[n][e], l[n][e]);
+            }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = n * 8 + t2 + e;
+                float2 w[KW];
+                float to = -CUDART_INF_F, sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < KW; ++k) { w[k] = s_part[k * ROWS + row]; to = fmaxf(to, w[k].x); }
+#pragma unroll
+                for (int k = 0; k < KW; ++k) sum += w[k].y * (w[k].x == to ? 1.f : ex2(w[k].x - to));
+                const float f = m[n][e] == to ? 1.f : ex2(m[n][e] - to);
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d) { o[d][n][e] *= f; o[d][n][e + 2] *= f; }
+                if (warp == 0 && g == 0) s_ml[row] = make_float2(to, sum);
+            }
+    }
+    // Sums over the lanes' keys: every lane then has the rows' sums
+    __device__ __forceinline__ void join_lanes() {
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+    }
+    // Puts (or adds) the columns [cb * HD / COLS, ..) of this warp's output to buf[row][ld]
+    __device__ __forceinline__ void put(float* buf, int ld, int, bool add) {
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float* at = buf + (n * 8 + t2 + (e & 1)) * ld + d * 16 + (e >> 1) * 8 + g;
+                    *at = add ? *at + o[d][n][e] : o[d][n][e];
+                }
+    }
+};
 
-    // ---- the queries of a (sequence, KV head, row block)
-    int rows = 0, m0 = 0;                                 // valid query rows of the block, its first row
-    int pos_a = 0, pos_b = 0;                             // last visible slot of this thread's two rows, -1: no such row
-    auto load_q = [&]() {
-        const int h = C.hr / a.RB, rb = C.hr - h * a.RB;
-        m0 = rb * a.rows_block;
-        rows = min(C.s.nb * a.G - m0, MT * 16);           // (may be < 0: a block of rows that this sequence does not have)
-        const uint16_t* q = a.q + (long long)C.b * a.q_sb;
-        for (int i = tid; i < MT * 16 * CH; i += NT) {
-            const int m = i / CH, c = i - m * CH;
-            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (m < rows && c < chunks) {
+// 17 to 64 query rows: queries on the M side, S = Q K^T and O = P V; the warps stand MT over the rows by 4 / MT over the keys.
+template <typename T, int HD, int ROWS> struct Wide {
+    using L = Tile<HD, ROWS>;
+    static constexpr int MT = L::MT, KW = 4 / MT, WK = TK / KW, CH = L::CH, QN = ROWS * CH / NT;
+    float o[HD / 8][4];              // (row g | g + 8, columns 2t, 2t + 1)
+    float m_a, m_b, l_a, l_b;        // of rows g, g + 8; sums of this thread's keys
+    uint4 q[QN];
+    int pos_a, pos_b;
+    int g, t2, warp, lane, wm, wk, tid_;
+
+    __device__ __forceinline__ void init(int tid) {
+        tid_ = tid; lane = tid & 31; warp = tid >> 5; g = lane >> 2; t2 = (lane & 3) * 2; wm = warp % MT; wk = warp / MT;
+    }
+    __device__ __forceinline__ void reset() {
+        m_a = m_b = -CUDART_INF_F;
+        l_a = l_b = 0.f;
+#pragma unroll
+        for (int n = 0; n < HD / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    }
+    __device__ __forceinline__ void read_q(const AttnArgs& a, const uint16_t* base, int h, int m0, int rows) {
+#pragma unroll
+        for (int k = 0; k < QN; ++k) {
+            const int i = tid_ + k * NT, m = i / CH, c = i - m * CH;
+            q[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (m < rows && c * 8 < a.kv.hd) {
                 const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-                w = __ldg(reinterpret_cast<const uint4*>(q + (long long)r * a.q_sr + (long long)hq * a.q_sh + c * 8));
+                q[k] = __ldg(reinterpret_cast<const uint4*>(base + (long long)r * a.q_sr + (long long)hq * a.q_sh + c * 8));
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(sm_q + L::at(m, c)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+        }
+    }
+    __device__ __forceinline__ void put_q(const AttnArgs& a, uint32_t sm_q, int first_pos, int m0, int rows) {
+#pragma unroll
+        for (int k = 0; k < QN; ++k) {
+            const int i = tid_ + k * NT, m = i / CH, c = i - m * CH;
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(sm_q + at<HD>(m, c)), "r"(q[k].x), "r"(q[k].y), "r"(q[k].z), "r"(q[k].w)
+                         : "memory");
         }
         const int ma = wm * 16 + g, mb = ma + 8;
-        pos_a = ma < rows ? C.s.len - C.s.nb + (m0 + ma) / a.G : -1;
-        pos_b = mb < rows ? C.s.len - C.s.nb + (m0 + mb) / a.G : -1;
-        __syncthreads();
-    };
-    load_q();
-
-    float o[HD / 8][4];
-    float m_a = -CUDART_INF_F, m_b = -CUDART_INF_F, l_a = 0.f, l_b = 0.f;
-#pragma unroll
-    for (int n = 0; n < HD / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-
-    int stage = 0;
-    int first_t = C.t;                                    // tile at which this block entered the head
-    for (int i = 0; i < count; ++i) {
-        cp_wait<S - 2>();
-        if constexpr (MT == 1) __syncwarp(); else __syncthreads();
-        {
-            int into = stage + S - 1;
-            if (into >= S) into -= S;
-            if (ahead < count) {
-                copy(off, into);
-                if (++ahead < count) { advance(a, P); off = look_up(P); }
-            }
-            cp_commit();
-        }
-        const uint32_t tk = sm + stage * 2 * L::BYTES, tv = tk + L::BYTES;
-        if (++stage == S) stage = 0;
-        const int j0 = (C.t < C.s.ns ? C.t : C.t + C.s.skip) * TK;
-        const int first_pos = C.s.len - C.s.nb, last_pos = C.s.len - 1;
-        // every slot of the tile is visible to every row
-        const bool inner = j0 + TK - 1 <= first_pos && (a.window <= 0 || j0 + TK <= a.sinks || j0 > last_pos - a.window);
-        auto sees = [&](int j, int pos) { return j <= pos && (a.window <= 0 || j > pos - a.window || j < a.sinks); };
-
-        // ---- scores of 16 rows x WK keys
+        pos_a = ma < rows ? first_pos + (m0 + ma) / a.G : -1;
+        pos_b = mb < rows ? first_pos + (m0 + mb) / a.G : -1;
+    }
+    __device__ __forceinline__ void tile(const AttnArgs& a, const TileAt& t, uint32_t sm_q, float* scores, int chunks) {
         float s[WK / 8][4];
 #pragma unroll
         for (int n = 0; n < WK / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        const uint32_t at_q = sm_q + at<HD>(wm * 16 + (lane & 15), lane >> 4);
+        const uint32_t at_k = t.k + at<HD>(wk * WK + (lane >> 4) * 8 + (lane & 7), (lane >> 3) & 1);
+        const uint32_t at_v = t.v + at<HD>(wk * WK + (lane & 15), lane >> 4);
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
             uint32_t qa[4];
-            ldsm4(qa, sm_q + L::at(wm * 16 + (lane & 15), ks * 2 + (lane >> 4)));
+            ldsm4(qa, at_q ^ (ks << 5));
 #pragma unroll
             for (int n = 0; n < WK / 8; n += 2) {
                 uint32_t kb[4];
-                ldsm4(kb, tk + L::at(wk * WK + (n + (lane >> 4)) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)));
+                ldsm4(kb, (at_k ^ (ks << 5)) + n * 8 * HD * 2);
                 mma<T>(s[n], qa, kb[0], kb[1]);
                 mma<T>(s[n + 1], qa, kb[2], kb[3]);
             }
@@ -325,31 +462,30 @@ __global__ void __launch_bounds__(NT, Tile<HD>::BLOCKS) attn_kernel(const AttnAr
         for (int n = 0; n < WK / 8; ++n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
-            if (!inner) {
-                const int j = j0 + wk * WK + n * 8 + t2;
-                if (!sees(j, pos_a)) s[n][0] = -CUDART_INF_F;
-                if (!sees(j + 1, pos_a)) s[n][1] = -CUDART_INF_F;
-                if (!sees(j, pos_b)) s[n][2] = -CUDART_INF_F;
-                if (!sees(j + 1, pos_b)) s[n][3] = -CUDART_INF_F;
+            if (!t.inner) {
+                const int j = t.j0 + wk * WK + n * 8 + t2;
+                if (!sees(a, j, pos_a)) s[n][0] = -CUDART_INF_F;
+                if (!sees(a, j + 1, pos_a)) s[n][1] = -CUDART_INF_F;
+                if (!sees(a, j, pos_b)) s[n][2] = -CUDART_INF_F;
+                if (!sees(a, j + 1, pos_b)) s[n][3] = -CUDART_INF_F;
             }
             x_a = fmaxf(x_a, fmaxf(s[n][0], s[n][1]));
             x_b = fmaxf(x_b, fmaxf(s[n][2], s[n][3]));
         }
-        if (a.scores) {
-            float* row = a.scores + (((long long)C.b * a.kv.Hkv + C.hr / a.RB) * (a.RB * a.rows_block) + m0 + wm * 16 + g) * a.score_ld +
-                         j0 + wk * WK + t2;
+        if (scores) {
+            float* row = scores + (wm * 16 + g) * a.score_ld + t.j0 + wk * WK + t2;
 #pragma unroll
             for (int n = 0; n < WK / 8; ++n) {
                 if (pos_a >= 0) *reinterpret_cast<float2*>(row + n * 8) = make_float2(s[n][0], s[n][1]);
                 if (pos_b >= 0) *reinterpret_cast<float2*>(row + 8 * a.score_ld + n * 8) = make_float2(s[n][2], s[n][3]);
             }
         }
+        if (__any_sync(0xffffffffu, x_a > m_a + RAISE || x_b > m_b + RAISE)) {
 #pragma unroll
-        for (int d = 1; d < 4; d <<= 1) {
-            x_a = fmaxf(x_a, __shfl_xor_sync(0xffffffffu, x_a, d));
-            x_b = fmaxf(x_b, __shfl_xor_sync(0xffffffffu, x_b, d));
-        }
-        if (__any_sync(0xffffffffu, x_a > m_a || x_b > m_b)) {            // (few tiles raise the maximum)
+            for (int d = 1; d < 4; d <<= 1) {
+                x_a = fmaxf(x_a, __shfl_xor_sync(0xffffffffu, x_a, d));
+                x_b = fmaxf(x_b, __shfl_xor_sync(0xffffffffu, x_b, d));
+            }
             const float n_a = fmaxf(m_a, x_a), n_b = fmaxf(m_b, x_b);
             const float f_a = m_a == n_a ? 1.f : ex2(m_a - n_a), f_b = m_b == n_b ? 1.f : ex2(m_b - n_b);
             m_a = n_a; m_b = n_b;
@@ -365,53 +501,30 @@ __global__ void __launch_bounds__(NT, Tile<HD>::BLOCKS) attn_kernel(const AttnAr
             l_a += s[n][0] + s[n][1];
             l_b += s[n][2] + s[n][3];
         }
-        // ---- values that only some rows see: an infinity or NaN among them must not reach the others as 0 * inf.  Such a value
-        // row is added to the rows that see it by hand and zeroed for the product.
-        if (!inner && C.s.nb > 1) {
-            bool odd = false;                             // a non-finite value in a row of this warp's share that not all see
-            for (int r = lane; r < RW; r += 32) {
-                const int j = j0 + warp * RW + r;
-                if (j <= last_pos && !(sees(j, first_pos) && sees(j, last_pos)))
-                    for (int c = 0; c < chunks; ++c) {
-                        uint32_t w[4];
-                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(tv + L::at(warp * RW + r, c)));
+        if (!t.inner && t.many && __syncthreads_or(odd_value<T, HD>(a, t, warp * 16, chunks, lane))) {     // (as in Narrow)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            odd = odd || (w[e] & Num<T>::kExp) == Num<T>::kExp || ((w[e] >> 16) & Num<T>::kExp) == Num<T>::kExp;
-                    }
-            }
-            const bool any = MT == 1 ? __any_sync(0xffffffffu, odd) : __syncthreads_or(odd);
-            if (any) {
-#pragma unroll
-                for (int k8 = 0; k8 < WK / 8; ++k8)
+            for (int k8 = 0; k8 < WK / 8; ++k8)
 #pragma unroll 1
-                    for (int e = 0; e < 8; ++e) {
-                        const int kk = k8 * 8 + e, j = j0 + wk * WK + kk;
-                        if (j > last_pos || (sees(j, first_pos) && sees(j, last_pos))) continue;
-                        const int from = (lane & ~3) | (e >> 1);
-                        const float p_a = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][1] : s[k8][0], from);
-                        const float p_b = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][3] : s[k8][2], from);
-                        const bool see_a = sees(j, pos_a), see_b = sees(j, pos_b);
+                for (int e = 0; e < 8; ++e) {
+                    const int kk = wk * WK + k8 * 8 + e, j = t.j0 + kk;
+                    if (!mixed(a, t, j)) continue;
+                    const int from = (lane & ~3) | (e >> 1);
+                    const float p_a = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][1] : s[k8][0], from);
+                    const float p_b = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][3] : s[k8][2], from);
+                    const bool see_a = sees(a, j, pos_a), see_b = sees(a, j, pos_b);
 #pragma unroll
-                        for (int n = 0; n < HD / 8; ++n) {
-                            uint32_t w;
-                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(tv + L::at(wk * WK + kk, n) + t2 * 2));
-                            const float2 v = Num<T>::unpack(w);
-                            if (see_a) { o[n][0] += p_a * v.x; o[n][1] += p_a * v.y; }
-                            if (see_b) { o[n][2] += p_b * v.x; o[n][3] += p_b * v.y; }
-                        }
+                    for (int n = 0; n < HD / 8; ++n) {
+                        uint32_t w;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(t.v + at<HD>(kk, n) + t2 * 2));
+                        const float2 v = Num<T>::unpack(w);
+                        if (see_a) { o[n][0] += p_a * v.x; o[n][1] += p_a * v.y; }
+                        if (see_b) { o[n][2] += p_b * v.x; o[n][3] += p_b * v.y; }
                     }
-                if constexpr (MT == 1) __syncwarp(); else __syncthreads();
-                for (int r = 0; r < RW; ++r) {
-                    const int j = j0 + warp * RW + r;
-                    if (j > last_pos || (sees(j, first_pos) && sees(j, last_pos))) continue;
-                    for (int c = lane; c < CH; c += 32)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + L::at(warp * RW + r, c)), "r"(0u) : "memory");
                 }
-                if constexpr (MT == 1) __syncwarp(); else __syncthreads();
-            }
+            __syncthreads();
+            zero_mixed<HD>(a, t, warp * 16, lane);
+            __syncthreads();
         }
-        // ---- o += P V, P as two terms
 #pragma unroll
         for (int ks = 0; ks < WK / 16; ++ks) {
             uint32_t ph[4], pl[4];
@@ -425,111 +538,535 @@ __global__ void __launch_bounds__(NT, Tile<HD>::BLOCKS) attn_kernel(const AttnAr
 #pragma unroll
             for (int n = 0; n < HD / 8; n += 2) {
                 uint32_t vb[4];
-                ldsm4t(vb, tv + L::at(wk * WK + ks * 16 + (lane & 15), n + (lane >> 4)));
+                ldsm4t(vb, (at_v ^ (n << 4)) + ks * 16 * HD * 2);
                 mma<T>(o[n], ph, vb[0], vb[1]);
                 mma<T>(o[n + 1], ph, vb[2], vb[3]);
                 mma<T>(o[n], pl, vb[0], vb[1]);
                 mma<T>(o[n + 1], pl, vb[2], vb[3]);
             }
         }
-
-        // ---- end of the head, or of this block's share of it
-        const bool last = i + 1 == count, head_end = C.t + 1 == C.s.nt;
-        if (!last && !head_end) { ++C.t; continue; }
-        const bool cut = first_t != 0 || !head_end;
-        // (a block's first piece goes to its place 0, one that begins inside its share to place 1)
-        const long long place = 2ll * blockIdx.x + (i - (C.t - first_t) > 0 ? 1 : 0);
+    }
+    __device__ __forceinline__ void join_warps(float2* s_part, float2* s_ml) {
 #pragma unroll
         for (int d = 1; d < 4; d <<= 1) {
             l_a += __shfl_xor_sync(0xffffffffu, l_a, d);
             l_b += __shfl_xor_sync(0xffffffffu, l_b, d);
         }
-        if (KW > 1) {
-            if ((lane & 3) == 0) {
-                s_m[warp][g] = m_a; s_m[warp][g + 8] = m_b;
-                s_l[warp][g] = l_a; s_l[warp][g + 8] = l_b;
+        if ((lane & 3) == 0) {
+            s_part[wk * ROWS + wm * 16 + g] = make_float2(m_a, l_a);
+            s_part[wk * ROWS + wm * 16 + g + 8] = make_float2(m_b, l_b);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int row = wm * 16 + g + half * 8;
+            float2 w[KW];
+            float to = -CUDART_INF_F, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) { w[k] = s_part[k * ROWS + row]; to = fmaxf(to, w[k].x); }
+#pragma unroll
+            for (int k = 0; k < KW; ++k) sum += w[k].y * (w[k].x == to ? 1.f : ex2(w[k].x - to));
+            const float mine = half ? m_b : m_a, f = mine == to ? 1.f : ex2(mine - to);
+#pragma unroll
+            for (int n = 0; n < HD / 8; ++n) { o[n][half * 2] *= f; o[n][half * 2 + 1] *= f; }
+            if (wk == 0 && (lane & 3) == 0) s_ml[row] = make_float2(to, sum);
+        }
+    }
+    __device__ __forceinline__ void put(float* buf, int ld, int cb, bool add) {
+        constexpr int NB = HD / 8 / L::COLS;
+        const bool all = ld == L::LDO;                    // every column
+#pragma unroll
+        for (int n = 0; n < HD / 8; ++n) {
+            if (!all && n / NB != cb) continue;
+            float* at = buf + (wm * 16 + g) * ld + (all ? n : n - cb * NB) * 8 + t2;
+#pragma unroll
+            for (int half = 0; half < 2; ++half, at += 8 * ld) {
+                float2 x = make_float2(o[n][half * 2], o[n][half * 2 + 1]);
+                if (add) { const float2 y = *reinterpret_cast<float2*>(at); x.x += y.x; x.y += y.y; }
+                *reinterpret_cast<float2*>(at) = x;
             }
+        }
+    }
+};
+
+// A warp brings 16 rows of keys and values (`apart` bytes further on): `off` is the offset of row lane & 15 in the pool, -1 where there
+// is nothing (zeros instead).
+template <int HD>
+__device__ __forceinline__ void copy_rows(const AttnArgs& a, long long off, uint32_t tile, int apart, int c_row, int c_col, int chunks,
+                                          long long v_from_k, long long pass_bytes) {
+    constexpr int CH = HD / 8, PASS = 32 / CH;
+    const uint32_t to = tile + c_row * HD * 2, piece = (c_col ^ c_row) << 4;      // (c_row < PASS <= 4: at() of row p * PASS + c_row)
+    auto dst = [&](int p) { return to + p * PASS * HD * 2 + (piece ^ (((p * PASS) & 7) << 4)); };
+    if (a.even && __all_sync(0xffffffffu, off >= 0)) {    // one run of a page
+        const char* src = reinterpret_cast<const char*>(a.kv.k + __shfl_sync(0xffffffffu, off, 0) + c_row * a.kv.slot_stride + c_col * 8);
+        const bool there = c_col < chunks;
+        if (!there) src = reinterpret_cast<const char*>(a.kv.k);
+#pragma unroll
+        for (int p = 0; p < 16 / PASS; ++p) {
+            cp16(dst(p), src, there);
+            cp16(dst(p) + apart, src + v_from_k, there);
+            if (there) src += pass_bytes;
+        }
+    } else {
+#pragma unroll 2
+        for (int p = 0; p < 16 / PASS; ++p) {
+            const long long o = __shfl_sync(0xffffffffu, off, p * PASS + c_row);
+            const bool there = o >= 0 && c_col < chunks;
+            const char* src = reinterpret_cast<const char*>(a.kv.k + (there ? o + c_col * 8 : 0));
+            cp16(dst(p), src, there);
+            cp16(dst(p) + apart, src + v_from_k, there);
+        }
+    }
+}
+
+constexpr int RW = 16;               // keys of a warp's tile
+
+// T: the cache's type; HD: head_dim rounded up to 64, 128 or 256; ROWS: query rows of a block.  LIST: the block has an even share of
+// the list of tiles; otherwise a cluster has a head, a block of it a share of the head's tiles, and the pieces are joined through
+// distributed shared memory.
+template <typename T, int HD, int ROWS, bool LIST>
+__global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const AttnArgs a) {
+    using L = Tile<HD, ROWS>;
+    using Core = typename std::conditional<(ROWS <= 16), Narrow<T, HD, ROWS>, Wide<T, HD, ROWS>>::type;
+    constexpr int KW = Core::KW, S = L::STAGES, CH = L::CH, PASS = 32 / CH;
+    constexpr bool OWN = ROWS <= 16;                      // a warp multiplies the rows that it has copied itself
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ float2 s_part[KW * ROWS];
+    __shared__ float2 s_ml[ROWS];                         // the block's; read by the cluster
+    __shared__ float2 s_all[LIST ? 1 : MAX_CLUSTER][LIST ? 1 : ROWS];
+    __shared__ long long s_scan[4];
+    __shared__ long long s_first[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t sm = (uint32_t)__cvta_generic_to_shared(smem);
+    const uint32_t sm_q = sm + S * 2 * L::BYTES;
+    float* const obuf = reinterpret_cast<float*>(smem + L::SMEM);
+    const int HR = a.kv.Hkv * a.RB, chunks = a.kv.hd >> 3;
+
+    pdl_wait();
+    pdl_trigger();
+    // ---- this block's share of the list
+    int count, rank = 0;
+    Cursor P;
+    if constexpr (!LIST) {
+        const int head = blockIdx.x / a.cluster;
+        rank = blockIdx.x - head * a.cluster;
+        P.b = head / HR;
+        P.hr = head - P.b * HR;
+        P.s = seq_of<TK>(a, P.b);
+        if (P.s.nt == 0) return;                          // (the whole cluster)
+        P.t = (int)((long long)P.s.nt * rank / a.cluster);
+        count = (int)((long long)P.s.nt * (rank + 1) / a.cluster) - P.t;
+    } else {
+        // first tiles of the sequences: up to 32 by one warp (every warp for itself), more by the block
+        const int lanes = a.B <= 32 ? 32 : NT, me = a.B <= 32 ? lane : tid;
+        const int each = (a.B + lanes - 1) / lanes, b0 = min(me * each, a.B), b1 = min(b0 + each, a.B);
+        long long mine = 0;
+        for (int b = b0; b < b1; ++b) mine += (long long)seq_of<TK>(a, b).nt * HR;
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        long long total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine;
+        if (a.B > 32) {
+            if (lane == 31) s_scan[warp] = incl;
             __syncthreads();
-            float n_a = m_a, n_b = m_b;
+            total = 0;
 #pragma unroll
-            for (int w = 0; w < KW; ++w) { n_a = fmaxf(n_a, s_m[w * MT + wm][g]); n_b = fmaxf(n_b, s_m[w * MT + wm][g + 8]); }
-            float t_a = 0.f, t_b = 0.f;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const float wa = s_m[w * MT + wm][g], wb = s_m[w * MT + wm][g + 8];
-                t_a += s_l[w * MT + wm][g] * (wa == n_a ? 1.f : ex2(wa - n_a));
-                t_b += s_l[w * MT + wm][g + 8] * (wb == n_b ? 1.f : ex2(wb - n_b));
-            }
-            const float f_a = m_a == n_a ? 1.f : ex2(m_a - n_a), f_b = m_b == n_b ? 1.f : ex2(m_b - n_b);
-#pragma unroll
-            for (int n = 0; n < HD / 8; ++n) { o[n][0] *= f_a; o[n][1] *= f_a; o[n][2] *= f_b; o[n][3] *= f_b; }
-            m_a = n_a; m_b = n_b; l_a = t_a; l_b = t_b;
-            // the warps over the keys add their outputs one after the other (of 32 rows, half the columns at a time)
-            constexpr int NB = HD / 8 / MT;
-#pragma unroll
-            for (int cb = 0; cb < MT; ++cb)
-#pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    if (wk == w) {
-                        float* ra = obuf + (wm * 16 + g) * (NB * 8) + t2;
-                        float* rb = ra + 8 * (NB * 8);
-#pragma unroll
-                        for (int k = 0; k < NB; ++k) {
-                            const int n = cb * NB + k;
-                            if (w > 0) {
-                                const float2 u = *reinterpret_cast<float2*>(ra + k * 8), v = *reinterpret_cast<float2*>(rb + k * 8);
-                                o[n][0] += u.x; o[n][1] += u.y; o[n][2] += v.x; o[n][3] += v.y;
-                            }
-                            if (w + 1 < KW) {
-                                *reinterpret_cast<float2*>(ra + k * 8) = make_float2(o[n][0], o[n][1]);
-                                *reinterpret_cast<float2*>(rb + k * 8) = make_float2(o[n][2], o[n][3]);
-                            }
-                        }
-                    }
-                    __syncthreads();
-                }
-        }
-        if (wk == KW - 1) {
-            const int h = C.hr / a.RB;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int m = wm * 16 + g + half * 8;
-                const float mm = half ? m_b : m_a, ll = half ? l_b : l_a;
-                if (m < rows) {
-                    if (cut) {
-                        float* dst = a.part_o + (place * a.rows_block + m) * HD + t2;
-#pragma unroll
-                        for (int n = 0; n < HD / 8; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][half * 2], o[n][half * 2 + 1]);
-                    } else {
-                        const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-                        uint16_t* dst = a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + t2;
-                        const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);       // (NaN stays NaN)
-#pragma unroll
-                        for (int n = 0; n < HD / 8; ++n)
-                            if (n < chunks)
-                                *reinterpret_cast<uint32_t*>(dst + n * 8) = Num<T>::pack(o[n][half * 2] * inv, o[n][half * 2 + 1] * inv);
-                        if (a.lse && (lane & 3) == 0)
-                            a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mm + log2f(ll)) * 0.6931471805599453f;
-                        if (a.weights && (lane & 3) == 0)
-                            a.row_lse2[((long long)C.b * HR + C.hr) * a.rows_block + m] = mm + log2f(ll);
-                    }
-                    if (cut && (lane & 3) == 0) a.part_ml[place * a.rows_block + m] = make_float2(mm, ll);
-                }
+            for (int w = 0; w < 4; ++w) {
+                if (w < warp) base += s_scan[w];
+                total += s_scan[w];
             }
         }
-        if (last) break;
-        advance(a, C);
-        first_t = 0;
-        m_a = m_b = -CUDART_INF_F;
-        l_a = l_b = 0.f;
-#pragma unroll
-        for (int n = 0; n < HD / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+        const long long per = (total + a.grid - 1) / a.grid, start = per * blockIdx.x, end = min(total, start + per);
+        if (blockIdx.x == 0 && (a.B > 32 || warp == 0)) { // for the second kernel
+            if (me == 0) { a.plan[0] = per; a.plan[a.B + 1] = total; }
+            long long x = base;
+            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += (long long)seq_of<TK>(a, b).nt * HR; }
+        }
+        if (start >= end) return;
+        count = (int)(end - start);
+        long long in = 0;
+        const bool here = start >= base && start < base + mine;
+        int b = b0;
+        if (here)
+            for (in = start - base;; ++b) {
+                const long long n = (long long)seq_of<TK>(a, b).nt * HR;
+                if (in < n) break;
+                in -= n;
+            }
+        if (a.B <= 32) {
+            const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+            b = __shfl_sync(0xffffffffu, b, from);
+            in = __shfl_sync(0xffffffffu, in, from);
+        } else {
+            if (here) { s_first[0] = b; s_first[1] = in; }
+            __syncthreads();
+            b = (int)s_first[0];
+            in = s_first[1];
+        }
+        P.b = b;
+        P.s = seq_of<TK>(a, b);
+        P.hr = (int)(in / P.s.nt);
+        P.t = (int)(in - (long long)P.hr * P.s.nt);
+    }
+    Cursor C = P;
+    Core core;
+    core.init(tid);
+    core.reset();
+    int rows = 0, m0 = 0;                                 // valid query rows of the block, its first row
+    auto read_q = [&]() {
+        const int h = C.hr / a.RB;
+        m0 = (C.hr - h * a.RB) * ROWS;
+        rows = min(C.s.nb * a.G - m0, ROWS);              // (may be < 0: a block of rows that this sequence does not have)
+        core.read_q(a, a.q + (long long)C.b * a.q_sb, h, m0, rows);
+    };
+    auto put_q = [&]() {
+        core.put_q(a, sm_q, C.s.len - C.s.nb, m0, rows);
         if (tid == 0 && a.status) {
             const int len = __ldg(a.lens + C.b);
             if (len < 0 || len > a.max_len) atomicOr(a.status + C.b, MTAD_ST_KV_OVERFLOW);
         }
-        __syncthreads();                                  // the old queries are no longer read
-        load_q();
+        if constexpr (!OWN) __syncthreads();
+    };
+
+    // ---- copies: a warp brings rows 16 * warp .. + 15 of a tile
+    // offset of the row of this lane (twice 16 of them) in the next tile to be copied, -1: nothing there (zeros instead)
+    auto look_up = [&](const Cursor& c) -> long long {
+        const int slot = (c.t < c.s.ns ? c.t : c.t + c.s.skip) * TK + warp * RW + (lane & 15);
+        const int hi = c.s.len - 1, lo = c.s.len - c.s.nb - a.window;     // the slots that some row sees
+        if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return -1;
+        const long long off = slot_offset(a.kv, a.kv.table + (long long)c.b * a.kv.table_stride, slot);
+        if (off < 0 && a.status) atomicOr(a.status + c.b, MTAD_ST_RANGE);
+        return off < 0 ? off : off + (long long)(c.hr / a.RB) * a.kv.head_stride;
+    };
+    const int c_row = lane / CH, c_col = lane % CH;       // this lane's row and piece in a request
+    const long long v_from_k = reinterpret_cast<const char*>(a.kv.v) - reinterpret_cast<const char*>(a.kv.k);
+    const long long pass_bytes = a.kv.slot_stride * (2 * PASS);
+    auto copy = [&](long long off, int stage) {
+        copy_rows<HD>(a, off, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks, v_from_k, pass_bytes);
+    };
+    int ahead = 0;                                        // tiles handed to the copies
+    long long off = count > 0 ? look_up(P) : -1;
+    read_q();
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) {
+        if (ahead < count) {
+            copy(off, s);
+            if (++ahead < count) { advance<TK>(a, P); off = look_up(P); }
+        }
+        cp_commit();
+    }
+    put_q();
+
+    int stage = 0;
+    int first_t = C.t;                                    // tile at which this block entered the head
+    for (int i = 0; i < count; ++i) {
+        cp_wait<S - 2>();
+        if constexpr (OWN) __syncwarp(); else __syncthreads();
+        {
+            int into = stage + S - 1;
+            if (into >= S) into -= S;
+            if (ahead < count) {
+                copy(off, into);
+                if (++ahead < count) { advance<TK>(a, P); off = look_up(P); }
+            }
+            cp_commit();
+        }
+        TileAt t;
+        t.k = sm + stage * 2 * L::BYTES;
+        t.v = t.k + L::BYTES;
+        if (++stage == S) stage = 0;
+        t.j0 = (C.t < C.s.ns ? C.t : C.t + C.s.skip) * TK;
+        t.first_pos = C.s.len - C.s.nb;
+        t.last_pos = C.s.len - 1;
+        t.inner = t.j0 + TK - 1 <= t.first_pos && (a.window <= 0 || t.j0 + TK <= a.sinks || t.j0 > t.last_pos - a.window);
+        if constexpr (OWN) {
+            t.k += warp * RW * HD * 2;
+            t.v += warp * RW * HD * 2;
+            t.j0 += warp * RW;
+        }
+        t.many = C.s.nb > 1;
+        float* const scores = a.scores ? a.scores + (((long long)C.b * a.kv.Hkv + C.hr / a.RB) * (a.RB * ROWS) + m0) * a.score_ld : nullptr;
+        core.tile(a, t, sm_q, scores, chunks);
+
+        // ---- end of the head, or of this block's share of it
+        ++C.t;
+        if constexpr (LIST) {
+            const bool last = i + 1 == count, head_end = C.t == C.s.nt;
+            if (!last && !head_end) continue;
+            const bool cut = first_t != 0 || !head_end;
+            // (a block's first piece goes to its place 0, one that begins inside its share to place 1)
+            const long long place = 2ll * blockIdx.x + (i + 1 > C.t - first_t ? 1 : 0);
+            core.join_warps(s_part, s_ml);
+            // the warps over the keys add their outputs one after the other, a part of the columns at a time
+            constexpr int W = HD / L::COLS;
+            const int h = C.hr / a.RB;
+#pragma unroll
+            for (int cb = 0; cb < L::COLS; ++cb) {
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    if (warp / L::MT == w) core.put(obuf, L::LDC, cb, w > 0);
+                    __syncthreads();
+                }
+                for (int k = tid; k < max(rows, 0) * (W / 4); k += NT) {
+                    const int m = k / (W / 4), c = (k - m * (W / 4)) * 4, d = cb * W + c;
+                    const float4 x = *reinterpret_cast<const float4*>(obuf + m * L::LDC + c);
+                    const float2 ml = s_ml[m];
+                    if (cut) {
+                        *reinterpret_cast<float4*>(a.part_o + (place * ROWS + m) * HD + d) = x;
+                        if (d == 0) a.part_ml[place * ROWS + m] = ml;
+                    } else {
+                        const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
+                        const float inv = inverse(ml.y);
+                        if (d < a.kv.hd)
+                            *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
+                                make_uint2(Num<T>::pack(x.x * inv, x.y * inv), Num<T>::pack(x.z * inv, x.w * inv));
+                        if (d == 0) {
+                            const float lse2 = ml.x + log2f(ml.y);
+                            if (a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = lse2 * LN2;
+                            if (a.weights) a.row_lse2[((long long)C.b * HR + C.hr) * ROWS + m] = lse2;
+                        }
+                    }
+                }
+                if (!(last && cb + 1 == L::COLS)) __syncthreads();
+            }
+            if (last) return;
+            C.t = C.s.nt - 1;
+            advance<TK>(a, C);
+            first_t = 0;
+            core.reset();
+            read_q();
+            put_q();
+        }
+    }
+    if constexpr (!LIST) {
+        // ---- the warps' outputs, brought to the block's reference, side by side where the tiles were
+        core.join_warps(s_part, s_ml);
+        float* const part = reinterpret_cast<float*>(smem);               // [KW][ROWS][LDO]
+        core.put(part + (warp / L::MT) * ROWS * L::LDO, L::LDO, 0, false);
+        cg::cluster_group cluster = cg::this_cluster();
+        const int CS = a.cluster;
+        if (CS > 1) cluster.sync(); else __syncthreads();
+        for (int i = tid; i < CS * ROWS; i += NT) {
+            const int k = i / ROWS, m = i - k * ROWS;
+            s_all[k][m] = CS > 1 ? *cluster.map_shared_rank(&s_ml[m], k) : s_ml[m];
+        }
+        __syncthreads();
+        // ---- a block adds the cluster's outputs of its share of (row, four columns)
+        const int h = C.hr / a.RB, per_row = a.kv.hd / 4, valid = max(rows, 0) * per_row;
+        for (int i = rank * NT + tid; i < valid; i += CS * NT) {
+            const int m = i / per_row, d = (i - m * per_row) * 4;
+            float mx = s_all[0][m].x, sum = 0.f;
+            for (int k = 1; k < CS; ++k) mx = fmaxf(mx, s_all[k][m].x);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int k = 0; k < CS; ++k) {
+                const float2 ml = s_all[k][m];
+                const float f = ml.x == mx ? 1.f : ex2(ml.x - mx);
+                sum += f * ml.y;
+                const float* src = CS > 1 ? cluster.map_shared_rank(part, k) : part;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    const float4 x = *reinterpret_cast<const float4*>(src + (w * ROWS + m) * L::LDO + d);
+                    acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
+                }
+            }
+            const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
+            const float inv = inverse(sum);
+            *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
+                make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
+            if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
+        }
+        // ---- weights of the slots of this block's tiles, from the scores that it wrote itself (one row block a head: see make_plan)
+        if (a.weights) {
+            float* const s_lse = reinterpret_cast<float*>(s_part);
+            if (tid < max(rows, 0)) {
+                float mx = s_all[0][tid].x, sum = 0.f;
+                for (int k = 1; k < CS; ++k) mx = fmaxf(mx, s_all[k][tid].x);
+                for (int k = 0; k < CS; ++k) sum += s_all[k][tid].y * (s_all[k][tid].x == mx ? 1.f : ex2(s_all[k][tid].x - mx));
+                s_lse[tid] = mx + log2f(sum);
+            }
+            __syncthreads();
+            const float* z = a.scores + ((long long)C.b * a.kv.Hkv + h) * ROWS * a.score_ld;
+            float* dst = a.weights + (long long)C.b * a.w_sb + (long long)h * a.w_sh;
+            for (int i = tid; i < count * TK; i += NT) {
+                const int tt = first_t + i / TK, j = (tt < C.s.ns ? tt : tt + C.s.skip) * TK + i % TK;
+                if (j >= C.s.len) continue;
+                float acc = 0.f;
+#pragma unroll 4
+                for (int m = 0; m < rows; ++m) {
+                    const float lse = s_lse[m];
+                    if (lse != -CUDART_INF_F) acc += ex2(z[(long long)m * a.score_ld + j] - lse);
+                }
+                dst[j] += acc;
+            }
+        }
+        if (CS > 1) cluster.sync();                       // (no block leaves while another reads its shared memory)
+    }
+}
+
+// Up to 16 query rows, the list cut over all warps of the GPU: a warp has an even share of the list of 16-key tiles and a ring of its own,
+// waits for nobody, and leaves its pieces of cut heads as they lie in its registers.  (With a block's four warps on one tile, their
+// outputs were added at the end of every share and head: 1.3 us each time in which the block's copies ran dry.)
+template <int HD, int ROWS> struct Ring {
+    static constexpr int BYTES = RW * HD * 2, STAGES = Tile<HD, ROWS>::STAGES;
+    static constexpr int SMEM = (NT / 32) * STAGES * 2 * BYTES;
+};
+template <typename T, int HD, int ROWS>
+__global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(const AttnArgs a) {
+    using L = Ring<HD, ROWS>;
+    using Core = Narrow<T, HD, ROWS>;
+    constexpr int S = L::STAGES, CH = HD / 8, PASS = 32 / CH;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.x * (NT / 32) + warp;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * S * 2 * L::BYTES;
+    const int Hkv = a.kv.Hkv, chunks = a.kv.hd >> 3;
+    pdl_wait();
+    pdl_trigger();
+    // ---- this warp's share of the list
+    int count;
+    Cursor P;
+    {
+        const int each = (a.B + 31) / 32, b0 = min(lane * each, a.B), b1 = min(b0 + each, a.B);
+        long long mine = 0;
+        for (int b = b0; b < b1; ++b) mine += (long long)seq_of<RW>(a, b).nt * Hkv;
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        const long long total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine, per = (total + a.grid - 1) / a.grid;
+        if (worker == 0) {                                // for the second kernel
+            if (lane == 0) a.plan[0] = per;
+            long long x = base;
+            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += (long long)seq_of<RW>(a, b).nt * Hkv; }
+        }
+        const long long start = per * worker;
+        if (start >= total) return;
+        count = (int)min(per, total - start);
+        const bool here = start >= base && start < base + mine;
+        int b = b0;
+        long long in = start - base;
+        if (here)
+            for (;; ++b) {
+                const long long n = (long long)seq_of<RW>(a, b).nt * Hkv;
+                if (in < n) break;
+                in -= n;
+            }
+        const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+        P.b = __shfl_sync(0xffffffffu, b, from);
+        in = __shfl_sync(0xffffffffu, in, from);
+        P.s = seq_of<RW>(a, P.b);
+        P.hr = (int)(in / P.s.nt);
+        P.t = (int)(in - (long long)P.hr * P.s.nt);
+    }
+    Cursor C = P;
+    Core core;
+    core.init(threadIdx.x);
+    core.reset();
+    int rows = 0;
+    auto read_q = [&]() {
+        rows = C.s.nb * a.G;
+        core.read_q(a, a.q + (long long)C.b * a.q_sb, C.hr, 0, rows);
+    };
+    auto put_q = [&]() {
+        core.put_q(a, 0, C.s.len - C.s.nb, 0, rows);
+        if (lane == 0 && a.status) {
+            const int len = __ldg(a.lens + C.b);
+            if (len < 0 || len > a.max_len) atomicOr(a.status + C.b, MTAD_ST_KV_OVERFLOW);
+        }
+    };
+    auto look_up = [&](const Cursor& c) -> long long {
+        const int slot = (c.t < c.s.ns ? c.t : c.t + c.s.skip) * RW + (lane & 15);
+        const int hi = c.s.len - 1, lo = c.s.len - c.s.nb - a.window;
+        if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return -1;
+        const long long off = slot_offset(a.kv, a.kv.table + (long long)c.b * a.kv.table_stride, slot);
+        if (off < 0 && a.status) atomicOr(a.status + c.b, MTAD_ST_RANGE);
+        return off < 0 ? off : off + (long long)c.hr * a.kv.head_stride;
+    };
+    const int c_row = lane / CH, c_col = lane % CH;
+    const long long v_from_k = reinterpret_cast<const char*>(a.kv.v) - reinterpret_cast<const char*>(a.kv.k);
+    const long long pass_bytes = a.kv.slot_stride * (2 * PASS);
+    auto copy = [&](long long off, int stage) { copy_rows<HD>(a, off, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks, v_from_k, pass_bytes); };
+    int ahead = 0;
+    long long off = look_up(P);
+    read_q();
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) {
+        if (ahead < count) {
+            copy(off, s);
+            if (++ahead < count) { advance<RW>(a, P); off = look_up(P); }
+        }
+        cp_commit();
+    }
+    put_q();
+    int stage = 0, first_t = C.t;
+    for (int i = 0; i < count; ++i) {
+        cp_wait<S - 2>();
+        __syncwarp();
+        if (ahead < count) {
+            copy(off, stage + S - 1 >= S ? stage - 1 : stage + S - 1);
+            if (++ahead < count) { advance<RW>(a, P); off = look_up(P); }
+        }
+        cp_commit();
+        TileAt t;
+        t.k = ring + stage * 2 * L::BYTES;
+        t.v = t.k + L::BYTES;
+        if (++stage == S) stage = 0;
+        t.j0 = (C.t < C.s.ns ? C.t : C.t + C.s.skip) * RW;
+        t.first_pos = C.s.len - C.s.nb;
+        t.last_pos = C.s.len - 1;
+        t.inner = t.j0 + RW - 1 <= t.first_pos && (a.window <= 0 || t.j0 + RW <= a.sinks || t.j0 > t.last_pos - a.window);
+        t.many = C.s.nb > 1;
+        const long long head = (long long)C.b * Hkv + C.hr;
+        core.tile(a, t, 0, a.scores ? a.scores + head * ROWS * a.score_ld : nullptr, chunks);
+        ++C.t;
+        const bool last = i + 1 == count, head_end = C.t == C.s.nt;
+        if (!last && !head_end) continue;
+        // ---- end of the head, or of this warp's share of it (first piece: place 0, one that begins inside the share: place 1)
+        const bool cut = first_t != 0 || !head_end;
+        const long long place = 2ll * worker + (i + 1 > C.t - first_t ? 1 : 0);
+        core.join_lanes();
+#pragma unroll
+        for (int n = 0; n < Core::N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int m = n * 8 + core.t2 + e;
+                if (m >= rows) continue;
+                if (cut) {
+                    float* dst = a.part_o + (place * ROWS + m) * HD + core.g;
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        dst[d * 16] = core.o[d][n][e];
+                        dst[d * 16 + 8] = core.o[d][n][e + 2];
+                    }
+                    if (core.g == 0) a.part_ml[place * ROWS + m] = make_float2(core.m[n][e], core.l[n][e]);
+                } else {
+                    const int r = m / a.G, hq = C.hr * a.G + m - r * a.G;
+                    T* dst = reinterpret_cast<T*>(a.out) + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + core.g;
+                    const float inv = inverse(core.l[n][e]);
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        if (d * 16 < a.kv.hd) dst[d * 16] = Num<T>::from(core.o[d][n][e] * inv);
+                        if (d * 16 + 8 < a.kv.hd) dst[d * 16 + 8] = Num<T>::from(core.o[d][n][e + 2] * inv);
+                    }
+                    if (core.g == 0) {
+                        const float lse2 = core.m[n][e] + log2f(core.l[n][e]);
+                        if (a.lse) a.lse[((long long)C.b * a.R + r) * (Hkv * a.G) + hq] = lse2 * LN2;
+                        if (a.weights) a.row_lse2[head * ROWS + m] = lse2;
+                    }
+                }
+            }
+        if (last) return;
+        C.t = C.s.nt - 1;
+        advance<RW>(a, C);
+        first_t = 0;
+        core.reset();
+        read_q();
+        put_q();
     }
 }
 
@@ -541,7 +1078,6 @@ struct Pieces {                      // the shares that hold a head's tiles
 };
 __device__ __forceinline__ Pieces pieces_of(const AttnArgs& a, const Seq& q, int b, int hr) {
     Pieces p;
-    if (a.whole) return Pieces{1, 0, 0, 1};
     p.per = a.plan[0];
     p.s = a.plan[1 + b] + (long long)hr * q.nt;
     p.c0 = p.s / p.per;
@@ -570,7 +1106,7 @@ constexpr int W_KEYS = 512;          // slots of a block that adds weights
 
 // Blocks [0, n_join): a warp per query row adds the pieces of its output.  Blocks beyond: the weights of W_KEYS slots of a KV head,
 // exp(score - lse) summed over the rows and the heads of the group and added to what is there.
-template <typename T, int HD>
+template <typename T, int HD, int UNIT>
 __global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, int groups) {
     constexpr int PER = HD / 32;     // columns of a lane
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, HR = a.kv.Hkv * a.RB;
@@ -578,7 +1114,7 @@ __global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, 
     pdl_wait();
     if ((int)blockIdx.x < n_join) {
         const int seg = blockIdx.x / groups, m = (blockIdx.x - seg * groups) * 4 + warp, b = seg / HR, hr = seg - b * HR;
-        const Seq q = seq_of(a, b);
+        const Seq q = seq_of<UNIT>(a, b);
         const int h = hr / a.RB, row = (hr - h * a.RB) * a.rows_block + m;
         if (q.nt == 0 || m >= a.rows_block || row >= q.nb * a.G) return;
         const Pieces p = pieces_of(a, q, b, hr);
@@ -600,25 +1136,25 @@ __global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, 
             }
         }
         const int r = row / a.G, hq = h * a.G + row - r * a.G;
-        const float inv = ml.y > 0.f ? 1.f / ml.y : (ml.y == 0.f ? 0.f : ml.y);
+        const float inv = inverse(ml.y);
         if (lane * PER < a.kv.hd) {
             uint16_t* dst = a.out + (long long)b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + lane * PER;
 #pragma unroll
             for (int k = 0; k < PER; k += 2) *reinterpret_cast<uint32_t*>(dst + k) = Num<T>::pack(acc[k] * inv, acc[k + 1] * inv);
         }
-        if (a.lse && lane == 0) a.lse[((long long)b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+        if (a.lse && lane == 0) a.lse[((long long)b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (ml.x + log2f(ml.y)) * LN2;
         return;
     }
     const int per_head = (a.max_len + W_KEYS - 1) / W_KEYS, w = blockIdx.x - n_join, bh = w / per_head, b = bh / a.kv.Hkv, h = bh - b * a.kv.Hkv;
     const int k0 = (w - bh * per_head) * W_KEYS;
-    const Seq q = seq_of(a, b);
+    const Seq q = seq_of<UNIT>(a, b);
     if (q.nt == 0 || k0 >= q.len) return;
     // slots of tiles that no row sees have no scores
     bool there[4];
     float acc[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int j = k0 + k * NT + tid, t = j / TK;
+        const int j = k0 + k * NT + tid, t = j / UNIT;
         there[k] = j < q.len && (t < q.ns || t >= q.ns + q.skip);
         acc[k] = 0.f;
     }
@@ -665,8 +1201,8 @@ struct Carve {
 };
 struct AttnPlan {
     AttnArgs a;
-    int HD, MT, grid;
-    long long max_tiles;
+    int HD, grid;
+    bool narrow;                     // the list is cut over warps
     size_t plan, part_o, part_ml, row_lse2, scores, bytes;
 };
 
@@ -697,56 +1233,87 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     a.weights = c->weights; a.w_sb = c->weights_stride_seq; a.w_sh = c->weights_stride_head;
     p->HD = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
     const int M = a.R * a.G;
-    p->MT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    a.rows_block = 16 * p->MT;
+    a.rows_block = M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : 64;
     a.RB = (M + a.rows_block - 1) / a.rows_block;
-    long long tiles = (a.max_len + TK - 1) / TK;
+    long long tiles = (a.max_len + TK - 1) / TK;          // of 64 keys
     if (a.window > 0) {
         const long long some = (long long)(a.sinks + TK - 1) / TK + ((long long)a.window + a.R + TK - 2) / TK + 1;
         tiles = some < tiles ? some : tiles;
     }
-    p->max_tiles = tiles;
     const long long heads = (long long)a.B * a.kv.Hkv * a.RB;
-    if (heads * tiles > 0x7fffffffll || heads * ((a.max_len + W_KEYS - 1) / W_KEYS) + heads * 16 > 0x7fffffffll) return MTAD_E_CAPACITY;
-    a.whole = tiles <= WHOLE_TILES;
-    // (workspace sizes are asked for without a device: the largest grid that the kernels run with)
+    if (heads * std::max(4 * tiles, (long long)MAX_CLUSTER) > 0x7fffffffll ||
+        heads * ((a.max_len + W_KEYS - 1) / W_KEYS) + heads * 16 > 0x7fffffffll) return MTAD_E_CAPACITY;
+    // (workspace sizes may be asked for without a device)
     int sms = 148, dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) {
-        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) sms = 148;
-    }
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) sms = 148;
     const long long fill = (long long)sms * (p->HD == 256 ? 1 : 2);
-    p->grid = (int)(a.whole ? heads : heads * tiles < fill ? heads * tiles : fill);
-    a.grid = p->grid;
+    // A cluster per head where that takes few tiles a block
+    int cs = 1;
+    while (cs < MAX_CLUSTER && cs < tiles && heads * cs * 2 <= fill) cs *= 2;
+    const bool list = (tiles + cs - 1) / cs > CLUSTER_TILES || (a.weights && a.RB > 1);
+    a.cluster = list ? 0 : cs;
+    a.even = kv->page_size % 16 == 0;
+    p->narrow = list && a.rows_block <= 16;
+    p->grid = (int)(list ? std::min(heads * tiles, fill) : heads * cs);
+    a.grid = p->narrow ? p->grid * (NT / 32) : p->grid;  // shares
     Carve w;
-    p->plan = w.take(a.whole ? 0 : sizeof(long long) * (a.B + 2));
-    p->part_o = w.take(a.whole ? 0 : sizeof(float) * 2 * (size_t)p->grid * a.rows_block * p->HD);
-    p->part_ml = w.take(a.whole ? 0 : sizeof(float2) * 2 * (size_t)p->grid * a.rows_block);
+    p->plan = w.take(list ? sizeof(long long) * (a.B + 2) : 0);
+    p->part_o = w.take(list ? sizeof(float) * 2 * (size_t)a.grid * a.rows_block * p->HD : 0);
+    p->part_ml = w.take(list ? sizeof(float2) * 2 * (size_t)a.grid * a.rows_block : 0);
     a.score_ld = a.weights ? (long long)((a.max_len + TK - 1) / TK) * TK : 0;
-    p->row_lse2 = w.take(a.weights ? sizeof(float) * heads * a.rows_block : 0);
+    p->row_lse2 = w.take(list && a.weights ? sizeof(float) * heads * a.rows_block : 0);
     p->scores = w.take(a.weights ? sizeof(float) * (size_t)heads * a.rows_block * a.score_ld : 0);
     p->bytes = w.off;
     return MTAD_OK;
 }
 
-template <typename T, int HD, int MT>
+template <typename T, int HD, int ROWS, bool LIST>
 cudaError_t launch_attn(const AttnPlan& p, cudaStream_t st) {
-    constexpr int smem = attn_smem<HD, MT>();
-    cudaError_t e = ops_smem<attn_kernel<T, HD, MT>>(smem);
+    constexpr int smem = Tile<HD, ROWS>::SMEM + (LIST ? Tile<HD, ROWS>::OBUF : 0);
+    const cudaError_t e = ops_smem<attn_kernel<T, HD, ROWS, LIST>>(smem);
     if (e != cudaSuccess) return e;
-    attn_kernel<T, HD, MT><<<p.grid, NT, smem, st>>>(p.a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(p.grid);
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = LIST ? 1 : p.a.cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = LIST ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, attn_kernel<T, HD, ROWS, LIST>, p.a);
+}
+template <typename T, int HD, int ROWS>
+cudaError_t launch_stream(const AttnPlan& p, cudaStream_t st) {
+    constexpr int smem = Ring<HD, ROWS>::SMEM;
+    const cudaError_t e = ops_smem<stream_kernel<T, HD, ROWS>>(smem);
+    return e != cudaSuccess ? e : launch_pdl(stream_kernel<T, HD, ROWS>, dim3(p.grid), dim3(NT), smem, st, true, p.a);
+}
+template <typename T, int HD, bool LIST>
+cudaError_t launch_rows(const AttnPlan& p, cudaStream_t st) {
+    switch (p.a.rows_block) {
+        case 8: if constexpr (LIST) return launch_stream<T, HD, 8>(p, st); else return launch_attn<T, HD, 8, LIST>(p, st);
+        case 16: if constexpr (LIST) return launch_stream<T, HD, 16>(p, st); else return launch_attn<T, HD, 16, LIST>(p, st);
+        case 32: return launch_attn<T, HD, 32, LIST>(p, st);
+        default: return launch_attn<T, HD, 64, LIST>(p, st);
+    }
 }
 template <typename T, int HD>
 cudaError_t launch_hd(const AttnPlan& p, cudaStream_t st) {
-    cudaError_t e = p.MT == 1 ? launch_attn<T, HD, 1>(p, st) : p.MT == 2 ? launch_attn<T, HD, 2>(p, st) : launch_attn<T, HD, 4>(p, st);
+    mtad_ops_count(1);
+    if (p.a.cluster) return launch_rows<T, HD, false>(p, st);
+    const cudaError_t e = launch_rows<T, HD, true>(p, st);
     if (e != cudaSuccess) return e;
     mtad_ops_count(1);
-    const int groups = (min(p.a.R * p.a.G, p.a.rows_block) + 3) / 4;
-    const int join = p.a.whole ? 0 : p.a.B * p.a.kv.Hkv * p.a.RB * groups;
+    const int groups = (std::min(p.a.R * p.a.G, p.a.rows_block) + 3) / 4;
+    const int join = p.a.B * p.a.kv.Hkv * p.a.RB * groups;
     const int add = p.a.weights ? p.a.B * p.a.kv.Hkv * ((p.a.max_len + W_KEYS - 1) / W_KEYS) : 0;
-    if (join + add == 0) return cudaSuccess;
-    mtad_ops_count(1);
-    return launch_pdl(join_kernel<T, HD>, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups);
+    return p.narrow ? launch_pdl(join_kernel<T, HD, RW>, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups)
+                    : launch_pdl(join_kernel<T, HD, TK>, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups);
 }
 template <typename T>
 cudaError_t launch_t(const AttnPlan& p, cudaStream_t st) {

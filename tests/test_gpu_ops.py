@@ -707,3 +707,40 @@ def test_a_run_of_them_together():
                 P["k"] = P["k"].gather(1, idx[..., None].expand(-1, -1, hd))
                 P["v"] = P["v"].gather(1, idx[..., None].expand(-1, -1, hd))
     assert evicted >= 2
+
+
+def test_calls_captured_behind_copies_and_joined_streams():
+    """A captured call right behind a copy, a fill and a second stream that joins: the graph's replay gives the eager call's results."""
+    c = Cache(40, [500, 90], 2, 64, 16)
+    q = queries(40, 2, 1, 4, 64, torch.bfloat16)
+    src, other = q.clone(), torch.zeros(1 << 20, device="cuda")
+    want = M.paged_attention(q, *c.args(), c.lens, max_len=500)
+    z, dr, tok, u, ua, logq = rows_of(41, 2, 3, 700, torch.float32)
+    res, eager = M.ResultBuffers(2, 3, 3), M.ResultBuffers(2, 3, 3)
+    M.accept_chain_spd(z, tok, dr, ua, u, eager)
+    scores = torch.rand(2, 2, 500, device="cuda")
+    kept0, new0 = M.paged_evict(*c.args(), c.lens, scores, 100, recent=10)
+    c = Cache(40, [500, 90], 2, 64, 16)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    main.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=main):
+        q.copy_(src)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            other.add_(1)
+        main.wait_stream(side)
+        out = M.paged_attention(q, *c.args(), c.lens, max_len=500)
+        res.buf.zero_()
+        M.accept_chain_spd(z, tok, dr, ua, u, res)
+        M.paged_append(None, c.k[c.table[:, :1].long()][:, :, :, 0], c.v[c.table[:, :1].long()][:, :, :, 0], *c.args(), torch.ones_like(c.lens))
+        kept, new = M.paged_evict(*c.args(), c.lens, scores, 100, recent=10)
+    q.zero_()
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(res.buf, eager.buf) and torch.equal(kept, kept0) and torch.equal(new, new0)
+    g.replay()
+    torch.cuda.synchronize()
+    c2 = Cache(40, [500, 90], 2, 64, 16)
+    assert torch.equal(M.paged_attention(q, *c2.args(), c2.lens, max_len=500), want) and out.shape == want.shape

@@ -14,7 +14,14 @@ from paper_2407_09722_b200 import ops
 def lib():
     from paper_2407_09722_b200.build import build
     build()
-    return ops._lib()
+    lib, P, KV = M.load_library(), C.c_void_p, C.POINTER(ops.PagedKV)
+    lib.mtad_paged_append.argtypes = [KV, C.POINTER(ops.PagedRows), P]
+    lib.mtad_paged_attention_workspace.argtypes = [KV, C.POINTER(ops.PagedAttn), C.POINTER(C.c_size_t)]
+    lib.mtad_paged_attention.argtypes = [KV, C.POINTER(ops.PagedAttn), P, C.c_size_t, P]
+    lib.mtad_paged_evict.argtypes = [KV, C.POINTER(ops.PagedEviction), P]
+    lib.mtad_accept_chain.argtypes = [C.POINTER(ops.AcceptRows), P, C.c_float, C.POINTER(Bn.Result), P]
+    lib.mtad_accept_chain_spd.argtypes = [C.POINTER(ops.AcceptRows), P, P, C.POINTER(Bn.Result), P]
+    return lib
 
 
 def _kv(**kw):
