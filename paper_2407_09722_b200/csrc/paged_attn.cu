@@ -18,6 +18,7 @@
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as two terms of the cache's type
 // (p and what its rounding left), so the 2^-9 of a bf16 probability does not reach the output; the output is rounded once.
 #include <cooperative_groups.h>
+#include <limits.h>
 #include <math_constants.h>
 
 #include <algorithm>
@@ -50,6 +51,7 @@ struct AttnArgs {
     int window, sinks, max_len;
     float scale2;                    // scale * log2(e)
     int even;                        // 16 neighbouring slots, the first a multiple of 16, lie in one page
+    int dense;                       // the slot stride where it is a row's length, else 0
     int cluster;                     // blocks of a head; 0: the list is cut evenly over the grid
     int grid;
     // workspace
@@ -207,6 +209,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
     static constexpr int N8 = ROWS / 8, KW = 4;
     float o[HD / 16][N8][4];         // (column g | g + 8, row 2t | 2t + 1)
     float m[N8][2], l[N8][2];        // reference (log2 domain) and sum (of this thread's keys) of rows 2t, 2t + 1
+    float over[N8][2], ref[N8][2];   // the score above which the reference is raised; the reference, 0 while there is none
     uint32_t q[HD / 16][N8][2];
     int pos[N8][2];                  // last visible slot, -1: no such row
     int g, t2, warp, lane;
@@ -215,8 +218,8 @@ template <typename T, int HD, int ROWS> struct Narrow {
     __device__ __forceinline__ void reset() {
 #pragma unroll
         for (int n = 0; n < N8; ++n) {
-            m[n][0] = m[n][1] = -CUDART_INF_F;
-            l[n][0] = l[n][1] = 0.f;
+            m[n][0] = m[n][1] = over[n][0] = over[n][1] = -CUDART_INF_F;
+            l[n][0] = l[n][1] = ref[n][0] = ref[n][1] = 0.f;
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) o[d][n][0] = o[d][n][1] = o[d][n][2] = o[d][n][3] = 0.f;
         }
@@ -257,14 +260,14 @@ template <typename T, int HD, int ROWS> struct Narrow {
 #pragma unroll
             for (int n = 0; n < N8; ++n) mma<T>(s[n], ka, q[k][n][0], q[k][n][1]);
         }
-        bool over = false;
+        bool raise = false;
 #pragma unroll
         for (int n = 0; n < N8; ++n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 s[n][e] *= a.scale2;
                 if (!t.inner && !sees(a, t.j0 + g + (e >> 1) * 8, pos[n][e & 1])) s[n][e] = -CUDART_INF_F;
-                over = over || s[n][e] > m[n][e & 1] + RAISE;
+                raise = raise || s[n][e] > over[n][e & 1];
             }
             if (scores) {
                 float* z = scores + (n * 8 + t2) * a.score_ld + t.j0 + g;
@@ -272,7 +275,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
                 if (pos[n][1] >= 0) { z[a.score_ld] = s[n][1]; z[a.score_ld + 8] = s[n][3]; }
             }
         }
-        if (__any_sync(0xffffffffu, over)) {
+        if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
             for (int n = 0; n < N8; ++n)
 #pragma unroll
@@ -282,6 +285,8 @@ template <typename T, int HD, int ROWS> struct Narrow {
                     for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
                     const float to = fmaxf(m[n][e], x), f = m[n][e] == to ? 1.f : ex2(m[n][e] - to);
                     m[n][e] = to;
+                    over[n][e] = to + RAISE;
+                    ref[n][e] = to == -CUDART_INF_F ? 0.f : to;
                     l[n][e] *= f;
 #pragma unroll
                     for (int d = 0; d < HD / 16; ++d) { o[d][n][e] *= f; o[d][n][e + 2] *= f; }
@@ -291,7 +296,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
         for (int n = 0; n < N8; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[n][e] = ex2(s[n][e] - (m[n][e & 1] == -CUDART_INF_F ? 0.f : m[n][e & 1]));
+                s[n][e] = ex2(s[n][e] - ref[n][e & 1]);
                 l[n][e & 1] += s[n][e];
             }
         // values that only some rows see: an infinity or NaN among them must not reach the others as 0 * inf.  Such a value row
@@ -589,32 +594,55 @@ template <typename T, int HD, int ROWS> struct Wide {
     }
 };
 
-// A warp brings 16 rows of keys and values (`apart` bytes further on): `off` is the offset of row lane & 15 in the pool, -1 where there
-// is nothing (zeros instead).
+// What a lane knows of its row (lane & 15) of the next 16 to be copied: the page id as it came from the table - used only when the copy is
+// made, a tile later, so that nobody waits for the load - and the slot in the page; id -1: no row sees the slot (zeros instead).
+struct Spot {
+    int id, in;
+};
+__device__ __forceinline__ Spot look_up(const AttnArgs& a, const Seq& s, int b, int slot) {
+    const int hi = s.len - 1, lo = s.len - s.nb - a.window;               // the slots that some row sees
+    if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return Spot{-1, 0};
+    const uint32_t p = div_by((uint32_t)slot, a.kv.page);
+    const int id = __ldg(a.kv.table + (long long)b * a.kv.table_stride + p);
+    return Spot{id == -1 ? INT_MIN : id, slot - (int)(p * a.kv.page.d)};
+}
+// A warp brings 16 rows of keys and values (`apart` bytes further on) of a KV head that begins at `head` of a page.
 template <int HD>
-__device__ __forceinline__ void copy_rows(const AttnArgs& a, long long off, uint32_t tile, int apart, int c_row, int c_col, int chunks,
-                                          long long v_from_k, long long pass_bytes) {
+__device__ __forceinline__ void copy_rows(const AttnArgs& a, const Spot& at_, int b, long long head, uint32_t tile, int apart, int c_row, int c_col,
+                                          int chunks) {
     constexpr int CH = HD / 8, PASS = 32 / CH;
     const uint32_t to = tile + c_row * HD * 2, piece = (c_col ^ c_row) << 4;      // (c_row < PASS <= 4: at() of row p * PASS + c_row)
     auto dst = [&](int p) { return to + p * PASS * HD * 2 + (piece ^ (((p * PASS) & 7) << 4)); };
-    if (a.even && __all_sync(0xffffffffu, off >= 0)) {    // one run of a page
-        const char* src = reinterpret_cast<const char*>(a.kv.k + __shfl_sync(0xffffffffu, off, 0) + c_row * a.kv.slot_stride + c_col * 8);
-        const bool there = c_col < chunks;
-        if (!there) src = reinterpret_cast<const char*>(a.kv.k);
+    const bool there = (unsigned)at_.id < (unsigned)a.kv.n_pages;
+    if (a.even && __all_sync(0xffffffffu, there)) {       // one run of a page
+        const long long e = (long long)__shfl_sync(0xffffffffu, at_.id, 0) * a.kv.page_stride + head +
+                            (__shfl_sync(0xffffffffu, at_.in, 0) + c_row) * a.kv.slot_stride + c_col * 8;
+        if (a.dense == HD) {                              // rows of just this length side by side: constant offsets
+            const uint16_t *k = a.kv.k + e, *v = a.kv.v + e;
 #pragma unroll
-        for (int p = 0; p < 16 / PASS; ++p) {
-            cp16(dst(p), src, there);
-            cp16(dst(p) + apart, src + v_from_k, there);
-            if (there) src += pass_bytes;
+            for (int p = 0; p < 16 / PASS; ++p) {
+                cp16(dst(p), k + p * PASS * HD, true);
+                cp16(dst(p) + apart, v + p * PASS * HD, true);
+            }
+        } else {
+            const bool in = c_col < chunks;
+            const uint16_t *k = a.kv.k + (in ? e : 0), *v = a.kv.v + (in ? e : 0);
+            const long long step = in ? PASS * a.kv.slot_stride : 0;
+#pragma unroll
+            for (int p = 0; p < 16 / PASS; ++p, k += step, v += step) {
+                cp16(dst(p), k, in);
+                cp16(dst(p) + apart, v, in);
+            }
         }
     } else {
+        if (!there && at_.id != -1 && a.status) atomicOr(a.status + b, MTAD_ST_RANGE);
+        const long long off = there ? (long long)at_.id * a.kv.page_stride + head + at_.in * a.kv.slot_stride : -1;
 #pragma unroll 2
         for (int p = 0; p < 16 / PASS; ++p) {
             const long long o = __shfl_sync(0xffffffffu, off, p * PASS + c_row);
-            const bool there = o >= 0 && c_col < chunks;
-            const char* src = reinterpret_cast<const char*>(a.kv.k + (there ? o + c_col * 8 : 0));
-            cp16(dst(p), src, there);
-            cp16(dst(p) + apart, src + v_from_k, there);
+            const bool in = o >= 0 && c_col < chunks;
+            cp16(dst(p), a.kv.k + (in ? o + c_col * 8 : 0), in);
+            cp16(dst(p) + apart, a.kv.v + (in ? o + c_col * 8 : 0), in);
         }
     }
 }
@@ -732,29 +760,20 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
     };
 
     // ---- copies: a warp brings rows 16 * warp .. + 15 of a tile
-    // offset of the row of this lane (twice 16 of them) in the next tile to be copied, -1: nothing there (zeros instead)
-    auto look_up = [&](const Cursor& c) -> long long {
-        const int slot = (c.t < c.s.ns ? c.t : c.t + c.s.skip) * TK + warp * RW + (lane & 15);
-        const int hi = c.s.len - 1, lo = c.s.len - c.s.nb - a.window;     // the slots that some row sees
-        if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return -1;
-        const long long off = slot_offset(a.kv, a.kv.table + (long long)c.b * a.kv.table_stride, slot);
-        if (off < 0 && a.status) atomicOr(a.status + c.b, MTAD_ST_RANGE);
-        return off < 0 ? off : off + (long long)(c.hr / a.RB) * a.kv.head_stride;
-    };
     const int c_row = lane / CH, c_col = lane % CH;       // this lane's row and piece in a request
-    const long long v_from_k = reinterpret_cast<const char*>(a.kv.v) - reinterpret_cast<const char*>(a.kv.k);
-    const long long pass_bytes = a.kv.slot_stride * (2 * PASS);
-    auto copy = [&](long long off, int stage) {
-        copy_rows<HD>(a, off, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks, v_from_k, pass_bytes);
+    auto find = [&](const Cursor& c) { return look_up(a, c.s, c.b, (c.t < c.s.ns ? c.t : c.t + c.s.skip) * TK + warp * RW + (lane & 15)); };
+    auto copy = [&](const Spot& spot, const Cursor& c, int stage) {
+        copy_rows<HD>(a, spot, c.b, (long long)(c.hr / a.RB) * a.kv.head_stride, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks);
     };
     int ahead = 0;                                        // tiles handed to the copies
-    long long off = count > 0 ? look_up(P) : -1;
+    Spot spot{-1, 0};
+    if (count > 0) spot = find(P);
     read_q();
 #pragma unroll
     for (int s = 0; s < S - 1; ++s) {
         if (ahead < count) {
-            copy(off, s);
-            if (++ahead < count) { advance<TK>(a, P); off = look_up(P); }
+            copy(spot, P, s);
+            if (++ahead < count) { advance<TK>(a, P); spot = find(P); }
         }
         cp_commit();
     }
@@ -769,8 +788,8 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
             int into = stage + S - 1;
             if (into >= S) into -= S;
             if (ahead < count) {
-                copy(off, into);
-                if (++ahead < count) { advance<TK>(a, P); off = look_up(P); }
+                copy(spot, P, into);
+                if (++ahead < count) { advance<TK>(a, P); spot = find(P); }
             }
             cp_commit();
         }
@@ -979,26 +998,19 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
             if (len < 0 || len > a.max_len) atomicOr(a.status + C.b, MTAD_ST_KV_OVERFLOW);
         }
     };
-    auto look_up = [&](const Cursor& c) -> long long {
-        const int slot = (c.t < c.s.ns ? c.t : c.t + c.s.skip) * RW + (lane & 15);
-        const int hi = c.s.len - 1, lo = c.s.len - c.s.nb - a.window;
-        if (slot > hi || (a.window > 0 && slot >= a.sinks && slot <= lo)) return -1;
-        const long long off = slot_offset(a.kv, a.kv.table + (long long)c.b * a.kv.table_stride, slot);
-        if (off < 0 && a.status) atomicOr(a.status + c.b, MTAD_ST_RANGE);
-        return off < 0 ? off : off + (long long)c.hr * a.kv.head_stride;
-    };
     const int c_row = lane / CH, c_col = lane % CH;
-    const long long v_from_k = reinterpret_cast<const char*>(a.kv.v) - reinterpret_cast<const char*>(a.kv.k);
-    const long long pass_bytes = a.kv.slot_stride * (2 * PASS);
-    auto copy = [&](long long off, int stage) { copy_rows<HD>(a, off, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks, v_from_k, pass_bytes); };
+    auto find = [&](const Cursor& c) { return look_up(a, c.s, c.b, (c.t < c.s.ns ? c.t : c.t + c.s.skip) * RW + (lane & 15)); };
+    auto copy = [&](const Spot& spot, const Cursor& c, int stage) {
+        copy_rows<HD>(a, spot, c.b, c.hr * a.kv.head_stride, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks);
+    };
     int ahead = 0;
-    long long off = look_up(P);
+    Spot spot = find(P);
     read_q();
 #pragma unroll
     for (int s = 0; s < S - 1; ++s) {
         if (ahead < count) {
-            copy(off, s);
-            if (++ahead < count) { advance<RW>(a, P); off = look_up(P); }
+            copy(spot, P, s);
+            if (++ahead < count) { advance<RW>(a, P); spot = find(P); }
         }
         cp_commit();
     }
@@ -1008,8 +1020,8 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
         cp_wait<S - 2>();
         __syncwarp();
         if (ahead < count) {
-            copy(off, stage + S - 1 >= S ? stage - 1 : stage + S - 1);
-            if (++ahead < count) { advance<RW>(a, P); off = look_up(P); }
+            copy(spot, P, stage + S - 1 >= S ? stage - 1 : stage + S - 1);
+            if (++ahead < count) { advance<RW>(a, P); spot = find(P); }
         }
         cp_commit();
         TileAt t;
@@ -1253,6 +1265,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     const bool list = (tiles + cs - 1) / cs > CLUSTER_TILES || (a.weights && a.RB > 1);
     a.cluster = list ? 0 : cs;
     a.even = kv->page_size % 16 == 0;
+    a.dense = kv->slot_stride == kv->head_dim ? kv->head_dim : 0;
     p->narrow = list && a.rows_block <= 16;
     p->grid = (int)(list ? std::min(heads * tiles, fill) : heads * cs);
     a.grid = p->narrow ? p->grid * (NT / 32) : p->grid;  // shares
