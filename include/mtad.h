@@ -398,7 +398,8 @@ int mtad_paged_attention(const mtad_paged_kv* kv, const mtad_paged_attn* call, v
  * with the largest scores stay, keep in all (first + recent <= keep; equal scores: the lower slot; NaN counts as larger than
  * every number).  They move to slots 0 .. keep - 1 in the order of their slots, so that the last tokens stay the last; slots from keep
  * on are left as they were.  kept[b][h][i] is the former slot of slot i (-1 from the new length on), scores_out[b][h][i] its score;
- * scores_out may be scores itself for max_len up to 327680 (MTAD_E_UNIMPLEMENTED beyond).  new_lens[b] = min(lens[b], keep); it
+ * scores_out may be scores itself for max_len up to 327680 (MTAD_E_UNIMPLEMENTED beyond; a zero then loses its sign and a NaN its
+ * bits).  new_lens[b] = min(lens[b], keep); it
  * must not be lens.  The pages of a sequence that is longer than keep must be its own: no other table row, nor another place
  * of its own row, may name them.  A length beyond max_len, or beyond what a table row can hold, is cut to it (MTAD_ST_KV_OVERFLOW); a row whose slot or whose new slot has no
  * page is not moved (MTAD_ST_RANGE). */

@@ -140,16 +140,20 @@ cudaError_t launch_append(const AppendArgs& a, const RopeTable& rope, int B, cud
 
 // ---------------------------------------------------------------------------------------------------------------
 // Eviction.  Of the `len` slots of a KV head the first `first`, the last `recent` and the largest scores stay, `keep` in all (lowest slot
-// first among equals), in the order of their slots; they move together to the front.
+// first among equals), in the order of their slots; they move together to the front.  Two launches:
 //
-// A cluster of eight blocks has a KV head.  Selection: each block holds an eighth of the scores in shared memory; the keep-th
-// largest is found by a radix descent over their ordered bits (11, 11 and 10 of them), histograms added up through distributed
-// shared memory; one more exchange of counts gives every block the place of its first kept slot.  Moving: the blocks
-// divide keys and values and the columns of a row, not the rows.  So a block walks its columns from the front with no one else in
-// its way: destination j lies at or before source kept[j], and what a later round reads lies behind everything that
-// earlier rounds wrote; only the reads of one round have to be over before its writes.  Bound by the bytes of what moves.
+// Selection, a cluster of one to eight blocks per KV head, as many as leave every SM one: each block holds its part of the scores in shared
+// memory; the keep-th largest is found by a radix descent over the ordered bits in which they differ (11 at a time), the histograms of a
+// cluster added up through distributed shared memory; one exchange of counts gives every block the place of its first kept slot.
+//
+// Moving.  The blocks of a head divide keys and values and the columns of a row, not the rows.  So a block walks its columns from the
+// front with no one else in its way: destination j lies at or before source kept[j], and what a later round reads lies behind
+// everything that earlier rounds wrote; only the reads of one round have to be over before its writes.  Bound by the bytes of what moves,
+// and by DRAM being read in pieces: whole rows of 256 bytes move 16 long contexts in 211 us, halves in 220, quarters 252, eighths 350 (and
+// clusters whose blocks take turns at the rows of a head, waiting for one another every round, in 236).
+// (One launch for both kept the blocks that move waiting in a selection that uses no bandwidth: 418 us for 16 long contexts, 36 for one.)
 
-constexpr int EV_CLUSTER = 8, EV_THREADS = 512, EV_BINS = 2048, EV_UNROLL = 8;
+constexpr int EV_THREADS = 1024, EV_BINS = 2048, EV_MAX_CLUSTER = 8;
 constexpr int EV_STAGE = 40 * 1024;  // scores that a block holds; more are read again from memory
 
 struct EvictArgs {
@@ -162,7 +166,7 @@ struct EvictArgs {
     float* scores_out;               // or null
     long long o_sb, o_sh;
     uint32_t* status;
-    int keep, first, recent, max_len, staged;
+    int keep, first, recent, max_len, staged, cluster;
 };
 
 // Order-preserving bits: larger score, larger key; -0 as +0; every NaN above all numbers.
@@ -172,176 +176,303 @@ __device__ __forceinline__ uint32_t score_key(float x) {
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ void __cluster_dims__(EV_CLUSTER, 1, 1) __launch_bounds__(EV_THREADS, 2) evict_kernel(const EvictArgs a) {
-    extern __shared__ float s_score[];
+__device__ __forceinline__ float key_score(uint32_t k) {
+    return k == 0xffffffffu ? CUDART_NAN_F : __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+}
+
+__global__ void __launch_bounds__(EV_THREADS) select_kernel(const EvictArgs a) {
+    extern __shared__ __align__(16) uint32_t s_key[];
     __shared__ __align__(16) uint32_t hist[3][EV_BINS];
     __shared__ int s_warp[EV_THREADS / 32], s_weq[EV_THREADS / 32];
     __shared__ int s_above, s_bin;
-    __shared__ int s_gt, s_eq, s_gap;                     // read by the cluster
+    __shared__ int s_gt, s_eq;                            // these and the histograms are read by the cluster
+    __shared__ uint32_t s_lo, s_hi;
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int bh = blockIdx.x / EV_CLUSTER, b = bh / a.kv.Hkv, h = bh - b * a.kv.Hkv;
+    const int CS = a.cluster, rank = CS > 1 ? (int)cluster.block_rank() : 0, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto sync = [&]() { if (CS > 1) cluster.sync(); else __syncthreads(); };
+    pdl_wait();
+    pdl_trigger();
+    const int bh = blockIdx.x / CS, b = bh / a.kv.Hkv, h = bh - b * a.kv.Hkv;
     const int raw = __ldg(a.lens + b), n = min(max(raw, 0), a.max_len);
     const float* z = a.scores + (long long)b * a.s_sb + (long long)h * a.s_sh;
     int32_t* kept = a.kept + (long long)bh * a.keep;
     float* zo = a.scores_out ? a.scores_out + (long long)b * a.o_sb + (long long)h * a.o_sh : nullptr;
     if (rank == 0 && h == 0 && tid == 0) {
         if (raw != n && a.status) atomicOr(a.status + b, MTAD_ST_KV_OVERFLOW);
+        a.new_lens[b] = min(n, a.keep);
     }
     if (n <= a.keep) {                                    // nothing to evict (the same for the whole cluster)
-        for (int j = rank * EV_THREADS + tid; j < a.keep; j += EV_CLUSTER * EV_THREADS) {
+        for (int j = rank * EV_THREADS + tid; j < a.keep; j += CS * EV_THREADS) {
             kept[j] = j < n ? j : -1;
             if (zo && j < n && zo != z) zo[j] = z[j];
         }
-        if (rank == 0 && h == 0 && tid == 0) a.new_lens[b] = n;
         return;
     }
-    const int chunk = (n + EV_CLUSTER - 1) / EV_CLUSTER, c0 = min(rank * chunk, n), c1 = min(c0 + chunk, n), mine = c1 - c0;
-    const int lo = a.first, hi = n - a.recent;            // slots outside [lo, hi) stay whatever their score
-    for (int i = tid; i < 3 * EV_BINS; i += EV_THREADS) (&hist[0][0])[i] = 0;
-    if (a.staged)
-        for (int i = tid; i < mine; i += EV_THREADS) s_score[i] = z[c0 + i];
+    const int chunk = ((n + CS - 1) / CS + 3) & ~3, c0 = min(rank * chunk, n), mine = min(chunk, n - c0);
+    // of this block's scores, those that may go: slots outside [first, n - recent) stay whatever their score
+    const int i_lo = min(max(a.first - c0, 0), mine), i_hi = max(min(n - a.recent - c0, mine), i_lo);
+    for (int i = tid; i < 3 * EV_BINS / 4; i += EV_THREADS) reinterpret_cast<uint4*>(&hist[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) { s_lo = 0xffffffffu; s_hi = 0; }
     __syncthreads();
-    auto score = [&](int i) { return a.staged ? s_score[i] : z[c0 + i]; };
+    // four neighbouring keys (of slots beyond the block's last: anything); keys(i, n): the element i * 4 + e is one that may go
+    auto four = [&](int i) -> uint4 {
+        if (a.staged) return reinterpret_cast<const uint4*>(s_key)[i];
+        uint32_t k[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k[e] = i * 4 + e < mine ? score_key(__ldg(z + c0 + i * 4 + e)) : 0;
+        return make_uint4(k[0], k[1], k[2], k[3]);
+    };
+    uint32_t k_lo = 0xffffffffu, k_hi = 0;                // smallest and largest key of those that may go
+    {
+        // eight requests of a thread in flight, of 16 bytes where the row begins on such a boundary
+        auto meet = [&](int i, const float4& w) {
+            const uint4 k = make_uint4(score_key(w.x), score_key(w.y), score_key(w.z), score_key(w.w));
+            if (i * 4 >= i_lo && i * 4 + 4 <= i_hi) {
+                k_lo = min(k_lo, min(min(k.x, k.y), min(k.z, k.w)));
+                k_hi = max(k_hi, max(max(k.x, k.y), max(k.z, k.w)));
+            } else {
+                const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i * 4 + e >= i_lo && i * 4 + e < i_hi) { k_lo = min(k_lo, key[e]); k_hi = max(k_hi, key[e]); }
+            }
+            if (a.staged) reinterpret_cast<uint4*>(s_key)[i] = k;
+        };
+        const float* from = z + c0;
+        const int nv = (reinterpret_cast<uintptr_t>(from) & 15) == 0 ? mine / 4 : 0;
+        for (int i0 = tid; i0 < nv; i0 += 8 * EV_THREADS) {
+            float4 w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i0 + u * EV_THREADS < nv) w[u] = __ldg(reinterpret_cast<const float4*>(from) + i0 + u * EV_THREADS);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i0 + u * EV_THREADS < nv) meet(i0 + u * EV_THREADS, w[u]);
+        }
+        for (int i0 = nv + tid; i0 * 4 < mine; i0 += 2 * EV_THREADS) {
+            float4 w[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = (i0 + u * EV_THREADS) * 4;
+                w[u].x = i < mine ? __ldg(from + i) : 0.f;
+                w[u].y = i + 1 < mine ? __ldg(from + i + 1) : 0.f;
+                w[u].z = i + 2 < mine ? __ldg(from + i + 2) : 0.f;
+                w[u].w = i + 3 < mine ? __ldg(from + i + 3) : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if ((i0 + u * EV_THREADS) * 4 < mine) meet(i0 + u * EV_THREADS, w[u]);
+        }
+    }
+    k_lo = __reduce_min_sync(0xffffffffu, k_lo);
+    k_hi = __reduce_max_sync(0xffffffffu, k_hi);
+    if (lane == 0) { atomicMin(&s_lo, k_lo); atomicMax(&s_hi, k_hi); }
+    sync();
+    k_lo = s_lo;
+    k_hi = s_hi;
+    if (CS > 1)
+        for (int k = 0; k < CS; ++k) { k_lo = min(k_lo, *cluster.map_shared_rank(&s_lo, k)); k_hi = max(k_hi, *cluster.map_shared_rank(&s_hi, k)); }
 
-    // ---- the key of the last slot that stays
-    uint32_t prefix = 0;
+    // ---- the key of the last slot that stays: bins over the keys' own range (of scores of a few magnitudes, most bits that they have in
+    // common would fall into a few bins of a fixed split, and their counters be fought for)
     int need = a.keep - a.first - a.recent;               // slots still to be found among those with this prefix
     const bool some = need > 0;
-#pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        if (some)
-            for (int i = tid; i < mine; i += EV_THREADS) {
-                const int j = c0 + i;
-                if (j < lo || j >= hi) continue;
-                const uint32_t key = score_key(score(i));
-                if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&hist[pass][(key >> shift) & ((1u << bits) - 1)], 1u);
+    uint32_t border = 0;                                  // key - k_lo of that slot, down to bit `shift`
+    int shift = 32 - __clz(k_hi - k_lo);
+#pragma unroll 1
+    for (int pass = 0; some && shift > 0; ++pass) {
+        const int from = shift, bits = min(shift, 11);
+        shift -= bits;
+        const uint32_t mask = (1u << bits) - 1, least = k_lo + border, width = from == 32 ? 0xffffffffu : (1u << from) - 1;
+        auto count = [&](uint32_t key) {                  // (keys with the prefix: least .. least + width)
+            const uint32_t d = key - least;
+            if (d <= width) atomicAdd(&hist[pass][(d >> shift) & mask], 1u);
+        };
+#pragma unroll 2
+        for (int i = (i_lo >> 2) + tid; i * 4 < i_hi; i += EV_THREADS) {
+            const uint4 k = four(i);
+            if (i * 4 >= i_lo && i * 4 + 4 <= i_hi) {
+                count(k.x); count(k.y); count(k.z); count(k.w);
+            } else {
+                if (i * 4 >= i_lo && i * 4 < i_hi) count(k.x);
+                if (i * 4 + 1 >= i_lo && i * 4 + 1 < i_hi) count(k.y);
+                if (i * 4 + 2 >= i_lo && i * 4 + 2 < i_hi) count(k.z);
+                if (i * 4 + 3 >= i_lo && i * 4 + 3 < i_hi) count(k.w);
             }
-        cluster.sync();
-        if (some) {
-            // bins from the top: thread t has the four below 2048 - 4 t
-            const int bin0 = EV_BINS - 4 * (tid + 1);
-            uint4 sum = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int k = 0; k < EV_CLUSTER; ++k) {
-                const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(&hist[pass][bin0], k));
-                sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
-            }
-            const int total = (int)(sum.x + sum.y + sum.z + sum.w);
-            int incl = total;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            if (lane == 31) s_warp[warp] = incl;
-            __syncthreads();
-            int before = incl - total;
-            for (int w = 0; w < warp; ++w) before += s_warp[w];
-            if (before < need && need <= before + total) {
-                const uint32_t c[4] = {sum.w, sum.z, sum.y, sum.x};
-                int at = before;
-                for (int k = 0; k < 4; ++k) {
-                    if (need <= at + (int)c[k]) { s_bin = bin0 + 3 - k; s_above = at; break; }
-                    at += (int)c[k];
-                }
-            }
-            __syncthreads();
-            prefix = (prefix << bits) | (uint32_t)s_bin;
-            need -= s_above;
-            __syncthreads();
         }
-    }
-    // ---- places: every thread has a run of neighbouring slots
-    const int run = (mine + EV_THREADS - 1) / EV_THREADS, i0 = min(tid * run, mine), i1 = min(i0 + run, mine);
-    int gt = 0, eq = 0, gap = 0x7fffffff;                  // that stay for certain, that lie on the border, first one that goes
-    for (int i = i0; i < i1; ++i) {
-        const int j = c0 + i;
-        if (j < lo || j >= hi) { ++gt; continue; }
-        if (!some) continue;
-        const uint32_t key = score_key(score(i));
-        gt += key > prefix;
-        eq += key == prefix;
-    }
-    int incl_g = gt, incl_e = eq;
+        sync();
+        // bins from the top: thread t has the two below 2048 - 2 t
+        const int bin0 = EV_BINS - 2 * (tid + 1);
+        uint2 sum = *reinterpret_cast<const uint2*>(&hist[pass][bin0]);
+        if (CS > 1) {
+            sum = make_uint2(0u, 0u);
+            for (int k = 0; k < CS; ++k) {
+                const uint2 x = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&hist[pass][bin0], k));
+                sum.x += x.x; sum.y += x.y;
+            }
+        }
+        const int total = (int)(sum.x + sum.y);
+        int incl = total;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, incl_g, o), y = __shfl_up_sync(0xffffffffu, incl_e, o);
-        if (lane >= o) { incl_g += x; incl_e += y; }
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (lane == 31) s_warp[warp] = incl;
+        __syncthreads();
+        const int w = s_warp[lane];                       // (32 warps)
+        const int before = incl - total + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+        if (before < need && need <= before + total) {
+            const bool upper = need <= before + (int)sum.y;
+            s_bin = bin0 + (upper ? 1 : 0);
+            s_above = before + (upper ? 0 : (int)sum.y);
+        }
+        __syncthreads();
+        border |= (uint32_t)s_bin << shift;
+        need -= s_above;
     }
-    if (lane == 31) { s_warp[warp] = incl_g; s_weq[warp] = incl_e; }
-    if (tid == 0) s_gap = 0x7fffffff;
+    border += k_lo;
+    // ---- places: a warp has a run of neighbouring slots
+    const int run = (mine + 128 * (EV_THREADS / 32) - 1) / (128 * (EV_THREADS / 32)) * 128, r0 = min(warp * run, mine), r1 = min(r0 + run, mine);
+    const int g0 = max(r0, i_lo), g1 = min(r1, i_hi);     // those of them that may go
+    int gt = 0, eq = 0;                                   // that stay for certain, that lie on the border
+    if (some) {
+#pragma unroll 2
+        for (int i = (g0 >> 2) + lane; i * 4 < g1; i += 32) {
+            const uint4 k = four(i);
+            const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+            const bool whole = i * 4 >= g0 && i * 4 + 4 <= g1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = whole || (i * 4 + e >= g0 && i * 4 + e < g1);
+                gt += in && key[e] > border;
+                eq += in && key[e] == border;
+            }
+        }
+        gt = __reduce_add_sync(0xffffffffu, gt);
+        eq = __reduce_add_sync(0xffffffffu, eq);
+    }
+    gt += (r1 - r0) - max(g1 - g0, 0);
+    __syncthreads();                                      // (the last pass's counts are no longer read)
+    if (lane == 0) { s_warp[warp] = gt; s_weq[warp] = eq; }
     __syncthreads();
-    int before_g = incl_g - gt, before_e = incl_e - eq, all_g = 0, all_e = 0;
-#pragma unroll
-    for (int w = 0; w < EV_THREADS / 32; ++w) {
-        if (w < warp) { before_g += s_warp[w]; before_e += s_weq[w]; }
-        all_g += s_warp[w];
-        all_e += s_weq[w];
-    }
-    if (tid == 0) { s_gt = all_g; s_eq = all_e; }
-    cluster.sync();
-    for (int k = 0; k < rank; ++k) { before_g += *cluster.map_shared_rank(&s_gt, k); before_e += *cluster.map_shared_rank(&s_eq, k); }
-    for (int i = i0; i < i1; ++i) {
-        const int j = c0 + i;
-        const float x = score(i);
-        const bool forced = j < lo || j >= hi;
-        const uint32_t key = score_key(x);
-        int at = -1;                                      // of those on the border the first `need` stay
-        if (forced || (some && key > prefix)) at = before_g++ + min(before_e, need);
-        else if (some && key == prefix) {
-            if (before_e < need) at = before_g + before_e;
-            ++before_e;
+    int before_g, before_e;
+    {
+        const int w = s_warp[lane], e = s_weq[lane];
+        before_g = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+        before_e = __reduce_add_sync(0xffffffffu, lane < warp ? e : 0);
+        if (CS > 1) {
+            const int all_g = __reduce_add_sync(0xffffffffu, w), all_e = __reduce_add_sync(0xffffffffu, e);
+            if (tid == 0) { s_gt = all_g; s_eq = all_e; }
+            cluster.sync();
+            for (int k = 0; k < rank; ++k) { before_g += *cluster.map_shared_rank(&s_gt, k); before_e += *cluster.map_shared_rank(&s_eq, k); }
         }
-        if (at >= 0) {
-            kept[at] = j;
-            if (zo) zo[at] = x;
+    }
+    auto put = [&](uint32_t at, int i, uint32_t key) {
+        kept[at] = c0 + i;
+        if (zo) {
+            float x = key_score(key);
+            // (what the key does not hold, a zero's sign and a NaN's bits, is read again; in place it may be overwritten by now)
+            if (key - 0x80000000u == 0u || key == 0xffffffffu) x = zo != z ? z[c0 + i] : x;
+            zo[at] = x;
+        }
+    };
+    for (int i = r0 + lane * 4; i - lane * 4 < r1; i += 128) {
+        const uint4 k = i < r1 ? four(i >> 2) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+        uint32_t sure = 0, edge = 0;                      // of the lane's four, a bit each
+        if (i >= g0 && i + 4 <= g1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sure |= key[e] > border ? 1u << e : 0u;
+                edge |= key[e] == border ? 1u << e : 0u;
+            }
+            if (!some) sure = edge = 0;
         } else {
-            gap = min(gap, j);
-        }
-    }
-    if (gap != 0x7fffffff) atomicMin(&s_gap, gap);
-    if (rank == 0 && h == 0 && tid == 0) a.new_lens[b] = a.keep;
-    cluster.sync();                                       // kept[] and the gaps of all blocks are there
-    int from = a.keep;
 #pragma unroll
-    for (int k = 0; k < EV_CLUSTER; ++k) from = min(from, *cluster.map_shared_rank(&s_gap, k));
-    cluster.sync();                                       // (no block leaves while another reads its shared memory)
+            for (int e = 0; e < 4; ++e) {
+                const bool may = i + e >= i_lo && i + e < i_hi;
+                if (i + e < r1 && (!may || (some && key[e] > border))) sure |= 1u << e;
+                if (i + e < r1 && may && some && key[e] == border) edge |= 1u << e;
+            }
+        }
+        const int own = __popc(sure) | __popc(edge) << 16;
+        int incl = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        const int all = __shfl_sync(0xffffffffu, incl, 31);
+        int g = before_g + ((incl - own) & 0xffff), eb = before_e + ((incl - own) >> 16);
+        if (all >> 16 == 0) {                             // nothing on the border: those that stay follow one another
+            uint32_t at = g + min(eb, need);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (sure >> e & 1) put(at++, i + e, key[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool is_sure = sure >> e & 1, is_edge = edge >> e & 1;
+                if (is_sure || (is_edge && eb < need)) put(g + min(eb, need), i + e, key[e]);          // of those on the border the first `need` stay
+                g += is_sure;
+                eb += is_edge;
+            }
+        }
+        before_g += all & 0xffff;
+        before_e += all >> 16;
+    }
+    if (CS > 1) cluster.sync();                           // (no block leaves while another reads its shared memory)
+}
 
-    // ---- moving: this block's tensor and columns
-    const int chunks = a.kv.hd >> 3, part = rank & 3, col0 = part * chunks / 4, cols = (part + 1) * chunks / 4 - col0;
+// A thread moves MV_UNROLL pieces of 16 bytes a round; offsets of a round's rows are worked out once per block, while the round before is in flight.
+constexpr int MV_THREADS = 512, MV_UNROLL = 8;
+constexpr int MV_SMEM = 3 * MV_THREADS * MV_UNROLL * (int)sizeof(longlong2);          // with parts of one piece
+__global__ void __launch_bounds__(MV_THREADS, 2) move_kernel(const EvictArgs a, int slices) {
+    extern __shared__ longlong2 s_off[];                  // [3][rows of a round] element offsets of source and destination, -1: not moved
+    const int part = blockIdx.x % slices, bh = blockIdx.x / slices, b = bh / a.kv.Hkv, h = bh - b * a.kv.Hkv, tid = threadIdx.x;
+    pdl_wait();
+    const int n = min(max(__ldg(a.lens + b), 0), a.max_len);
+    if (n <= a.keep) return;
+    const int half = slices >> 1, chunks = a.kv.hd >> 3, q = part % half, col0 = q * chunks / half, cols = (q + 1) * chunks / half - col0;
     if (cols == 0) return;
-    uint16_t* base = ((rank >> 2) ? a.kv.v : a.kv.k) + (long long)h * a.kv.head_stride;
+    const int32_t* kept = a.kept + (long long)bh * a.keep;
     const int32_t* row = a.kv.table + (long long)b * a.kv.table_stride;
-    const int rows = EV_THREADS / cols, rr = tid / cols, cc = (col0 + tid - rr * cols) * 8;
+    uint16_t* base = (part >= half ? a.kv.v : a.kv.k) + (long long)h * a.kv.head_stride;
+    const int rows = MV_THREADS / cols, round = rows * MV_UNROLL, rr = tid / cols, cc = (col0 + tid - rr * cols) * 8;
     const bool on = rr < rows;
     bool bad = false;
-    for (int j0 = from; j0 < a.keep; j0 += rows * EV_UNROLL) {
-        int src[EV_UNROLL];
-        long long so[EV_UNROLL], d_o[EV_UNROLL];
-        uint4 w[EV_UNROLL];
-#pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u) {
-            const int j = j0 + u * rows + rr;
-            src[u] = on && j < a.keep ? kept[j] : -1;
-        }
-#pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u) {
-            so[u] = d_o[u] = -1;
-            if (src[u] >= 0) {
-                so[u] = slot_offset(a.kv, row, src[u]);
-                d_o[u] = slot_offset(a.kv, row, j0 + u * rows + rr);
-                bad = bad || so[u] < 0 || d_o[u] < 0;
+    auto work_out = [&](int j0, longlong2* to) {
+        for (int i = tid; i < round; i += MV_THREADS) {
+            const int j = j0 + i, src = j < a.keep ? __ldg(kept + j) : -1;
+            longlong2 x = make_longlong2(-1, -1);
+            if (src > j) {                                // (the first ones stay where they are)
+                x.x = slot_offset(a.kv, row, src);
+                x.y = slot_offset(a.kv, row, j);
+                if (x.x < 0 || x.y < 0) { bad = true; x.x = -1; }
             }
+            to[i] = x;
         }
+    };
+    work_out(0, s_off);
+    __syncthreads();
+    int at = 0;
+    for (int j0 = 0; j0 < a.keep; j0 += round) {
+        const longlong2* off = s_off + at * round + rr;
+        uint4 w[MV_UNROLL];
 #pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u)
-            if (so[u] >= 0) w[u] = *reinterpret_cast<const uint4*>(base + so[u] + cc);
-        __syncthreads();
+        for (int u = 0; u < MV_UNROLL; ++u) {
+            const long long so = on ? off[u * rows].x : -1;
+            if (so >= 0) w[u] = *reinterpret_cast<const uint4*>(base + so + cc);
+        }
+        at = at == 2 ? 0 : at + 1;
+        if (j0 + round < a.keep) work_out(j0 + round, s_off + at * round);
+        __syncthreads();                                  // the round's reads are over, the next offsets are there
 #pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u)
-            if (so[u] >= 0 && d_o[u] >= 0) *reinterpret_cast<uint4*>(base + d_o[u] + cc) = w[u];
+        for (int u = 0; u < MV_UNROLL; ++u) {
+            const longlong2 x = on ? off[u * rows] : make_longlong2(-1, -1);
+            if (x.x >= 0) *reinterpret_cast<uint4*>(base + x.y + cc) = w[u];
+        }
     }
     if (bad && a.status) atomicOr(a.status + b, MTAD_ST_RANGE);
 }
@@ -416,15 +547,44 @@ int mtad_paged_evict(const mtad_paged_kv* kv, const mtad_paged_eviction* c, void
     a.status = c->status;
     a.keep = c->keep; a.first = c->first; a.recent = c->recent;
     a.max_len = (int)std::min((long long)c->max_len, (long long)kv->max_pages * kv->page_size);
-    const int chunk = (a.max_len + EV_CLUSTER - 1) / EV_CLUSTER;
+    int sms = 148, dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) sms = 148;
+    const int heads = c->batch * a.kv.Hkv;
+    a.cluster = 1;
+    while (a.cluster < EV_MAX_CLUSTER && (a.max_len > a.cluster * EV_STAGE || (heads * a.cluster * 2 <= sms && a.max_len > a.cluster * 4 * EV_THREADS)))
+        a.cluster *= 2;
+    const int chunk = ((a.max_len + a.cluster - 1) / a.cluster + 3) & ~3;
     a.staged = chunk <= EV_STAGE;
     if (!a.staged && c->scores_out == c->scores) return MTAD_E_UNIMPLEMENTED;      // read again after places are written
     const int smem = a.staged ? chunk * (int)sizeof(float) : 0;
-    cudaError_t e = ops_smem<evict_kernel>(EV_STAGE * (int)sizeof(float));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = ops_smem<select_kernel>(EV_STAGE * (int)sizeof(float));
     if (e == cudaSuccess) {
-        evict_kernel<<<c->batch * a.kv.Hkv * EV_CLUSTER, EV_THREADS, smem, static_cast<cudaStream_t>(stream)>>>(a);
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(heads * a.cluster);
+        cfg.blockDim = dim3(EV_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = a.cluster;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, select_kernel, a);
         mtad_ops_count(1);
-        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess && a.max_len > a.keep) {
+        // two tensors; parts of a row only where SMs would go without a block
+        int slices = 2;
+        while (slices < 16 && heads * slices < sms) slices *= 2;
+        // (a part of a row has at least one piece of 16 bytes where it has any)
+        const int least = std::max(kv->head_dim / 8 * 2 / slices, 1);
+        e = ops_smem<move_kernel>(MV_SMEM);
+        if (e == cudaSuccess) e = launch_pdl(move_kernel, dim3(heads * slices), dim3(MV_THREADS), (size_t)MV_SMEM / least, st, true, a, slices);
+        mtad_ops_count(1);
     }
     return ops_status(e);
 }
