@@ -23,9 +23,9 @@ namespace mtad {
 
 namespace {
 
-constexpr int AC_CLUSTER = 8, AC_THREADS = 512, AC_WARPS = AC_THREADS / 32;
+constexpr int AC_CLUSTER = 8;
 constexpr int AC_ROWS = 2 * MTAD_MAX_DEPTH + 1, AC_PARTS = 8;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct AcceptRowsArgs {
     const void *z, *q;               // target rows [B, gamma + 1, V], auxiliary rows [B, gamma, V] or null (threshold rule)
@@ -37,8 +37,10 @@ struct AcceptRowsArgs {
     mtad_result out;
 };
 
+// Statistics of logits over the temperature, in powers of two: x = z * c, c = log2(e) / temperature.  The reference is a whole number not
+// below the largest x, so x - ref is one fused multiply-add whose only rounding is the result's: no bias enters a sum of many.
 struct Stat {
-    float m, s;                      // sum of exp(x - m)
+    float m, s;                      // reference, sum of 2^(x - m)
 };
 __device__ __forceinline__ float ex2a(float x) {
     float y;
@@ -48,19 +50,25 @@ __device__ __forceinline__ float ex2a(float x) {
 __device__ __forceinline__ Stat merge(const Stat& a, const Stat& b) {
     const float m = fmaxf(a.m, b.m);
     if (m == -CUDART_INF_F) return Stat{m, a.s + b.s};    // (sums of 0, or NaN)
-    return Stat{m, a.s * (a.m == m ? 1.f : ex2a((a.m - m) * LOG2E)) + b.s * (b.m == m ? 1.f : ex2a((b.m - m) * LOG2E))};
+    return Stat{m, a.s * (a.m == m ? 1.f : ex2a(a.m - m)) + b.s * (b.m == m ? 1.f : ex2a(b.m - m))};
 }
+// N logits, the largest of them (times a positive c) known
 template <int N>
-__device__ __forceinline__ void take(Stat& st, const float (&x)[N]) {
-    float m = st.m;
+__device__ __forceinline__ void take(Stat& st, const float (&z)[N], float top, float c) {
+    const float x = top * c;
+    if (x > st.m) {
+        const float m = ceilf(x);
+        st.s *= st.m == -CUDART_INF_F ? 0.f : ex2a(st.m - m);
+        st.m = m;
+    }
+    const float r = st.m == -CUDART_INF_F ? 0.f : st.m;
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-    if (m > st.m) { st.s *= st.m == -CUDART_INF_F ? 0.f : ex2a((st.m - m) * LOG2E); st.m = m; }
-    const float r = m == -CUDART_INF_F ? 0.f : m;
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) s += ex2a((x[i] - r) * LOG2E);
-    st.s += s;
+    for (int i = 0; i < N; ++i) {
+        const float e = ex2a(fmaf(z[i], c, -r));
+        if (i & 1) s1 += e; else s0 += e;
+    }
+    st.s += s0 + s1;
 }
 
 template <typename T> struct Row;
@@ -70,7 +78,14 @@ template <> struct Row<float> {
         x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
     }
     static __device__ __forceinline__ float one(float x) { return x; }
+    static __device__ __forceinline__ uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+    static __device__ __forceinline__ float top(const uint4& w) {
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
 };
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> { using type = __nv_bfloat162; };
+template <> struct Pair<__half> { using type = __half2; };
 template <typename T> struct Row16 {
     static constexpr int N = 8;
     static __device__ __forceinline__ void vec(const uint4& w, float (&x)[8]) {
@@ -82,60 +97,126 @@ template <typename T> struct Row16 {
         }
     }
     static __device__ __forceinline__ float one(T x) { return Num<T>::to(x); }
+    static __device__ __forceinline__ uint4 nothing() {                  // -infinity, eight times
+        constexpr uint32_t w = (0x8000u | Num<T>::kExp) * 0x10001u;
+        return make_uint4(w, w, w, w);
+    }
+    // the largest of eight, two at a time (NaN is passed over: it shows in the sum)
+    static __device__ __forceinline__ float top(const uint4& w) {
+        using P = typename Pair<T>::type;
+        const P* p = reinterpret_cast<const P*>(&w);
+        const P m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+        const float2 f = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(&m));
+        return fmaxf(f.x, f.y);
+    }
 };
 template <> struct Row<__nv_bfloat16> : Row16<__nv_bfloat16> {};
 template <> struct Row<__half> : Row16<__half> {};
 
-// Statistics of elements [v0, v1) of a row, times mul, by one warp: 16-byte loads, four in flight a lane; what lies before the
+// Two fp32 at a time
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
+    return x;
+}
+__device__ __forceinline__ float2 halves(uint64_t x) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(x));
+    return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+
+// Statistics of elements [v0, v1) of a row, by one warp: 16-byte loads, U in flight a lane; what lies before the
 // first 16-byte boundary and behind the last (rows of odd vocabularies begin anywhere) one by one.
+// A lane's reference is the largest of its first load, kept to the end: a sum of 2^(x - ref) is as exact with terms up to 2^90 as with
+// terms up to 1, and looking for the largest of every load took longer than the exponentials.  Where the sum leaves that range (an
+// element more than 2^90 above the first ones, or all of them far below; a row that begins with masked tokens), the warp goes through
+// its elements again with a running maximum.
 template <typename T>
-__device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float mul, int lane) {
+__device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float c, int lane) {
     constexpr int N = Row<T>::N, U = 4;
-    Stat st{-CUDART_INF_F, 0.f};
     const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row + v0) & 15)) & 15) / (int)sizeof(T);
     const int a0 = min(v0 + skip, v1), nv = (v1 - a0) / N, tail = a0 + nv * N;
     const uint4* p = reinterpret_cast<const uint4*>(row + a0);
-    for (int i = lane; i < nv; i += 32 * U) {
+    const uint64_t cc = pair(c, c);
+    Stat st{0.f, 0.f};
+    uint64_t s0 = 0, s1 = 0, ref = 0;
+    bool any = false;
+    for (int i = lane; i - lane < nv; i += 32 * U) {
         uint4 w[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * 32 < nv) w[u] = __ldg(p + i + u * 32);
+        for (int u = 0; u < U; ++u)                       // (past the end: no weight)
+            w[u] = i + u * 32 < nv ? __ldg(p + i + u * 32) : Row<T>::nothing();
+        if (i == lane) {
+            const float m = ceilf(Row<T>::top(w[0]) * c);
+            any = i < nv;
+            st.m = isfinite(m) ? m : 0.f;
+            ref = pair(-st.m, -st.m);
+        }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * 32 < nv) {
-                float x[N];
-                Row<T>::vec(w[u], x);
+        for (int u = 0; u < U; ++u) {
+            float z[N];
+            Row<T>::vec(w[u], z);
 #pragma unroll
-                for (int k = 0; k < N; ++k) x[k] *= mul;
-                take<N>(st, x);
+            for (int k = 0; k < N; k += 4) {
+                const float2 x = halves(fma2(pair(z[k], z[k + 1]), cc, ref)), y = halves(fma2(pair(z[k + 2], z[k + 3]), cc, ref));
+                s0 = add2(s0, pair(ex2a(x.x), ex2a(x.y)));
+                s1 = add2(s1, pair(ex2a(y.x), ex2a(y.y)));
             }
+        }
     }
-    for (int v = v0 + lane; v < a0; v += 32) { const float x[1] = {Row<T>::one(row[v]) * mul}; take<1>(st, x); }
-    for (int v = tail + lane; v < v1; v += 32) { const float x[1] = {Row<T>::one(row[v]) * mul}; take<1>(st, x); }
+    const float2 t = halves(add2(s0, s1));
+    st.s = t.x + t.y;
+    if (__any_sync(0xffffffffu, any && !(st.s >= 0x1p-60f && st.s <= 0x1p90f))) {
+        st = Stat{-CUDART_INF_F, 0.f};
+        for (int i = lane; i < nv; i += 32) {
+            const uint4 w = __ldg(p + i);
+            float z[N];
+            Row<T>::vec(w, z);
+            take<N>(st, z, Row<T>::top(w), c);
+        }
+    } else if (!any) {
+        st = Stat{-CUDART_INF_F, 0.f};
+    }
+    for (int v = v0 + lane; v < a0; v += 32) { const float z[1] = {Row<T>::one(row[v])}; take<1>(st, z, z[0], c); }
+    for (int v = tail + lane; v < v1; v += 32) { const float z[1] = {Row<T>::one(row[v])}; take<1>(st, z, z[0], c); }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) st = merge(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o)});
     return st;
 }
 
-struct Best {                        // best candidate of the draw, and of a draw from p alone
-    float y, y2;
-    int v, v2;
+struct Best {
+    float y;
+    int v;
 };
-__device__ __forceinline__ void better(Best& a, float y, int v, float y2, int v2) {
+__device__ __forceinline__ void better(Best& a, float y, int v) {
     if (y > a.y || (y == a.y && v < a.v)) { a.y = y; a.v = v; }
-    if (y2 > a.y2 || (y2 == a.y2 && v2 < a.v2)) { a.y2 = y2; a.v2 = v2; }
 }
 
-template <typename T>
-__global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(AC_THREADS, 2) accept_rows_kernel(const AcceptRowsArgs a) {
+// THREADS: 512 where clusters are few and latency counts, 256 where they fill the GPU (more of them at work at once)
+template <typename T, int THREADS>
+__global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 / THREADS) accept_rows_kernel(const AcceptRowsArgs a) {
+    constexpr int WARPS = THREADS / 32;
+    constexpr bool few = THREADS == 512;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), b = blockIdx.x / AC_CLUSTER, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ Stat s_part[AC_ROWS * AC_PARTS];
     __shared__ Stat s_row[AC_ROWS];                       // read by the cluster
-    __shared__ Best s_best[AC_WARPS], s_block;            // s_block: read by the cluster
+    __shared__ Best s_best[WARPS], s_block;            // s_block: read by the cluster
     __shared__ float s_lse[AC_ROWS];
     __shared__ int s_eta;
     const int D = a.gamma, V = a.V;
+    pdl_wait();
+    pdl_trigger();
     const int given = a.n_draft ? __ldg(a.n_draft + b) : D, g = min(max(given, 0), D);
     const bool spd = a.q != nullptr;
     const int rows = g + 1 + (spd ? g : 0);
@@ -158,12 +239,26 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(AC_THREADS,
         }
         if (__any_sync(0xffffffffu, bad)) bits |= MTAD_ST_BAD_TOKEN;
     }
+    if (few) {                                            // (the draw's uniforms are on their way into the L2 meanwhile)
+        const float* u = a.u_last + (long long)b * V;
+        for (int v = v0 + tid * 32; v < v1; v += THREADS * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(u + v));
+    }
     // ---- log-sum-exp of every row
-    const int parts = min(AC_PARTS, max(1, (v1 - v0) / (Row<T>::N * 128))), step = (v1 - v0 + parts - 1) / parts;
-    for (int t = warp; t < rows * parts; t += AC_WARPS) {
+    // (as many parts of a row as leave the fewest warps idle in the last round, none of less than two loads a lane)
+    int parts = 1;
+    {
+        float best = 0.f;
+        const int most = min(AC_PARTS, max(1, (v1 - v0) / (Row<T>::N * 64)));
+        for (int p = 1; p <= most; ++p) {
+            const float use = (float)(rows * p) / (float)((rows * p + WARPS - 1) / WARPS * WARPS);
+            if (use > best + 0.02f) { best = use; parts = p; }
+        }
+    }
+    const int step = ((v1 - v0 + parts - 1) / parts + Row<T>::N - 1) / Row<T>::N * Row<T>::N;
+    for (int t = warp; t < rows * parts; t += WARPS) {
         const int r = t / parts, p = t - r * parts, e0 = min(v0 + p * step, v1), e1 = min(e0 + step, v1);
-        const Stat st = r <= g ? row_stat<T>(z + (long long)r * a.z_sr, e0, e1, a.z_mul, lane)
-                               : row_stat<T>(q + (long long)(r - g - 1) * a.q_sr, e0, e1, a.q_mul, lane);
+        const Stat st = r <= g ? row_stat<T>(z + (long long)r * a.z_sr, e0, e1, a.z_mul * LOG2E, lane)
+                               : row_stat<T>(q + (long long)(r - g - 1) * a.q_sr, e0, e1, a.q_mul * LOG2E, lane);
         if (lane == 0) s_part[t] = st;
     }
     __syncthreads();
@@ -176,7 +271,7 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(AC_THREADS,
     if (tid < rows) {
         Stat st = *cluster.map_shared_rank(&s_row[tid], 0);
         for (int k = 1; k < AC_CLUSTER; ++k) st = merge(st, *cluster.map_shared_rank(&s_row[tid], k));
-        s_lse[tid] = st.m + logf(st.s);
+        s_lse[tid] = (st.m + log2f(st.s)) * LN2;
     }
     __syncthreads();
     // ---- the accepted prefix (warp 0 of every block; the first block writes)
@@ -235,48 +330,97 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(AC_THREADS,
     }
     __syncthreads();
     const int eta = s_eta;
-    // ---- the last token: this block's share of the vocabulary
-    Best best{-CUDART_INF_F, -CUDART_INF_F, 0x7fffffff, 0x7fffffff};
-    if (eta >= 0) {                                       // (the same in every block of the cluster)
+    // ---- the last token: this block's share of the vocabulary.  w_v / -log u_v with its logarithm in full precision; -log u is taken only
+    // where the weight could still win, that is where w > best * (1 - u) (-log u >= 1 - u).
+    Best best{-CUDART_INF_F, 0x7fffffff};
+    auto search = [&](bool rest) {
         const T* row = z + (long long)eta * a.z_sr;
-        const bool rest = spd && eta < g;
         const T* qrow = rest ? q + (long long)eta * a.q_sr : row;
-        const float lse = s_lse[eta], lse_q = rest ? s_lse[g + 1 + eta] : 0.f;
+        const float cz = a.z_mul * LOG2E, cq = a.q_mul * LOG2E;
+        const float rz = s_lse[eta] * LOG2E, rq = rest ? s_lse[g + 1 + eta] * LOG2E : 0.f;
         const float* u = a.u_last + (long long)b * V;
-#pragma unroll 4
-        for (int v = v0 + tid; v < v1; v += AC_THREADS) {
-            const float p = ex2a((Row<T>::one(row[v]) * a.z_mul - lse) * LOG2E);
-            const float e = -logf(__ldg(u + v));
-            float w = p;
-            if (rest) w = fmaxf(p - ex2a((Row<T>::one(qrow[v]) * a.q_mul - lse_q) * LOG2E), 0.f);
-            // (a weight of zero is no candidate)
-            better(best, w > 0.f ? w / e : -CUDART_INF_F, w > 0.f ? v : 0x7fffffff, p > 0.f ? p / e : -CUDART_INF_F, p > 0.f ? v : 0x7fffffff);
+        float lead = 0.f;                                 // the best that this warp has seen
+        auto look = [&](float x, float y, float un, int v) {
+            const float w = ex2a(fmaf(x, cz, -rz)) - ex2a(fmaf(y, cq, -rq));
+            if (w > 0.f && !(w < lead * (1.f - un))) better(best, w / -logf(un), v);
+        };
+        auto share = [&]() { lead = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(best.y, 0.f)))); };
+        constexpr int N = Row<T>::N;
+        const bool even = ((reinterpret_cast<uintptr_t>(row + v0) | reinterpret_cast<uintptr_t>(qrow + v0) | reinterpret_cast<uintptr_t>(u + v0)) & 15) == 0;
+        const int nv = even ? (v1 - v0) / N : 0;          // 16-byte loads where all three rows allow them
+        for (int i = tid; i - tid < nv; i += 2 * THREADS) {
+            uint4 x[2], y[2];
+            float4 un[2][N / 4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int at = i + k * THREADS;
+                x[k] = at < nv ? __ldg(reinterpret_cast<const uint4*>(row + v0) + at) : Row<T>::nothing();
+                y[k] = rest && at < nv ? __ldg(reinterpret_cast<const uint4*>(qrow + v0) + at) : Row<T>::nothing();
+#pragma unroll
+                for (int h = 0; h < N / 4; ++h)
+                    un[k][h] = at < nv ? __ldg(reinterpret_cast<const float4*>(u + v0) + at * (N / 4) + h) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float zx[N], zy[N];
+                Row<T>::vec(x[k], zx);
+                Row<T>::vec(y[k], zy);
+                const int v = v0 + (i + k * THREADS) * N;
+#pragma unroll
+                for (int h = 0; h < N / 4; ++h) {
+                    look(zx[4 * h], zy[4 * h], un[k][h].x, v + 4 * h);
+                    look(zx[4 * h + 1], zy[4 * h + 1], un[k][h].y, v + 4 * h + 1);
+                    look(zx[4 * h + 2], zy[4 * h + 2], un[k][h].z, v + 4 * h + 2);
+                    look(zx[4 * h + 3], zy[4 * h + 3], un[k][h].w, v + 4 * h + 3);
+                }
+                share();
+            }
+        }
+        constexpr int U = 4;
+        for (int v = v0 + nv * N + tid; v - tid < v1; v += U * THREADS) {
+            float x[U], y[U], un[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const bool in = v + k * THREADS < v1;
+                x[k] = in ? Row<T>::one(row[v + k * THREADS]) : -CUDART_INF_F;
+                y[k] = rest && in ? Row<T>::one(qrow[v + k * THREADS]) : -CUDART_INF_F;
+                un[k] = in ? __ldg(u + v + k * THREADS) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) look(x[k], y[k], un[k], v + k * THREADS);
+            share();
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float y = __shfl_xor_sync(0xffffffffu, best.y, o), y2 = __shfl_xor_sync(0xffffffffu, best.y2, o);
-            const int v = __shfl_xor_sync(0xffffffffu, best.v, o), v2 = __shfl_xor_sync(0xffffffffu, best.v2, o);
-            better(best, y, v, y2, v2);
+        for (int o = 16; o > 0; o >>= 1) better(best, __shfl_xor_sync(0xffffffffu, best.y, o), __shfl_xor_sync(0xffffffffu, best.v, o));
+        if (lane == 0) s_best[warp] = best;
+        __syncthreads();
+        if (warp == 0) {
+            best = lane < WARPS ? s_best[lane] : Best{-CUDART_INF_F, 0x7fffffff};
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) better(best, __shfl_xor_sync(0xffffffffu, best.y, o), __shfl_xor_sync(0xffffffffu, best.v, o));
+            if (lane == 0) s_block = best;
         }
-    }
-    if (lane == 0) s_best[warp] = best;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < AC_WARPS; ++w) better(best, s_best[w].y, s_best[w].v, s_best[w].y2, s_best[w].v2);
-        s_block = best;
-    }
-    cluster.sync();
-    if (rank == 0 && tid == 0 && eta >= 0) {
-        for (int k = 1; k < AC_CLUSTER; ++k) {
+        cluster.sync();
+        best = Best{-CUDART_INF_F, 0x7fffffff};
+#pragma unroll
+        for (int k = 0; k < AC_CLUSTER; ++k) {
             const Best c = *cluster.map_shared_rank(&s_block, k);
-            better(best, c.y, c.v, c.y2, c.v2);
+            better(best, c.y, c.v);
         }
-        // (no mass left where p and q agree to the last bit: a draw from p)
-        const int t = best.v != 0x7fffffff ? best.v : best.v2 != 0x7fffffff ? best.v2 : 0;
-        a.out.out_tok[(long long)b * (D + 1) + eta] = t;
-        a.out.out_lp[(long long)b * (D + 1) + eta] = Row<T>::one(z[(long long)eta * a.z_sr + t]) * a.z_mul - s_lse[eta];
+    };
+    if (eta >= 0) {                                       // (the same in every block of the cluster)
+        search(spd && eta < g);
+        if (best.v == 0x7fffffff) {                       // no mass left where p and q agree to the last bit: a draw from p
+            cluster.sync();
+            search(false);
+        }
+        if (rank == 0 && tid == 0) {
+            const int t = best.v != 0x7fffffff ? best.v : 0;
+            a.out.out_tok[(long long)b * (D + 1) + eta] = t;
+            a.out.out_lp[(long long)b * (D + 1) + eta] = Row<T>::one(z[(long long)eta * a.z_sr + t]) * a.z_mul - s_lse[eta];
+        }
     }
-    cluster.sync();                                       // (no block leaves while the first reads its candidates)
+    cluster.sync();                                       // (no block leaves while another reads its shared memory)
 }
 
 int accept_rows(const mtad_accept_rows* c, const float* draft_logq, float log_tau, const void* q, const float* u_accept,
@@ -300,11 +444,12 @@ int accept_rows(const mtad_accept_rows* c, const float* draft_logq, float log_ta
     a.out = *out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const dim3 grid(c->batch * AC_CLUSTER);
-    if (c->dtype == MTAD_F32) accept_rows_kernel<float><<<grid, AC_THREADS, 0, st>>>(a);
-    else if (c->dtype == MTAD_BF16) accept_rows_kernel<__nv_bfloat16><<<grid, AC_THREADS, 0, st>>>(a);
-    else accept_rows_kernel<__half><<<grid, AC_THREADS, 0, st>>>(a);
     mtad_ops_count(1);
-    return ops_status(cudaGetLastError());
+    const bool few = c->batch * AC_CLUSTER <= 296;
+    auto launch = [&](auto wide, auto slim) { return few ? launch_pdl(wide, grid, dim3(512), 0, st, true, a) : launch_pdl(slim, grid, dim3(256), 0, st, true, a); };
+    return ops_status(c->dtype == MTAD_F32    ? launch(accept_rows_kernel<float, 512>, accept_rows_kernel<float, 256>)
+                      : c->dtype == MTAD_BF16 ? launch(accept_rows_kernel<__nv_bfloat16, 512>, accept_rows_kernel<__nv_bfloat16, 256>)
+                                              : launch(accept_rows_kernel<__half, 512>, accept_rows_kernel<__half, 256>));
 }
 
 }  // namespace
