@@ -143,7 +143,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // its elements again with a running maximum.
 template <typename T>
 __device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float c, int lane) {
-    constexpr int N = Row<T>::N, U = 4;
+    constexpr int N = Row<T>::N, U = 2;
     const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row + v0) & 15)) & 15) / (int)sizeof(T);
     const int a0 = min(v0 + skip, v1), nv = (v1 - a0) / N, tail = a0 + nv * N;
     const uint4* p = reinterpret_cast<const uint4*>(row + a0);
@@ -151,17 +151,20 @@ __device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float c, 
     Stat st{0.f, 0.f};
     uint64_t s0 = 0, s1 = 0, ref = 0;
     bool any = false;
-    for (int i = lane; i - lane < nv; i += 32 * U) {
-        uint4 w[U];
+    uint4 w[U], next[U];                                  // (the next loads are on their way while these are added)
+    auto load = [&](int i, uint4 (&to)[U]) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)                       // (past the end: no weight)
-            w[u] = i + u * 32 < nv ? __ldg(p + i + u * 32) : Row<T>::nothing();
-        if (i == lane) {
-            const float m = ceilf(Row<T>::top(w[0]) * c);
-            any = i < nv;
-            st.m = isfinite(m) ? m : 0.f;
-            ref = pair(-st.m, -st.m);
-        }
+        for (int u = 0; u < U; ++u) to[u] = i + u * 32 < nv ? __ldg(p + i + u * 32) : Row<T>::nothing();      // (past the end: no weight)
+    };
+    load(lane, w);
+    if (lane < nv) {
+        const float m = ceilf(Row<T>::top(w[0]) * c);
+        any = true;
+        st.m = isfinite(m) ? m : 0.f;
+        ref = pair(-st.m, -st.m);
+    }
+    for (int i = lane; i - lane < nv; i += 32 * U) {
+        load(i + 32 * U, next);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float z[N];
@@ -173,6 +176,8 @@ __device__ __forceinline__ Stat row_stat(const T* row, int v0, int v1, float c, 
                 s1 = add2(s1, pair(ex2a(y.x), ex2a(y.y)));
             }
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = next[u];
     }
     const float2 t = halves(add2(s0, s1));
     st.s = t.x + t.y;
@@ -244,14 +249,14 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 10
         for (int v = v0 + tid * 32; v < v1; v += THREADS * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(u + v));
     }
     // ---- log-sum-exp of every row
-    // (as many parts of a row as leave the fewest warps idle in the last round, none of less than two loads a lane)
+    // (as few parts of a row as keep most warps at work in the last round, none of less than two loads a lane)
     int parts = 1;
     {
         float best = 0.f;
         const int most = min(AC_PARTS, max(1, (v1 - v0) / (Row<T>::N * 64)));
         for (int p = 1; p <= most; ++p) {
             const float use = (float)(rows * p) / (float)((rows * p + WARPS - 1) / WARPS * WARPS);
-            if (use > best + 0.02f) { best = use; parts = p; }
+            if (best < 0.9f && use > best + 0.02f) { best = use; parts = p; }
         }
     }
     const int step = ((v1 - v0 + parts - 1) / parts + Row<T>::N - 1) / Row<T>::N * Row<T>::N;
