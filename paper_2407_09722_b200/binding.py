@@ -1,4 +1,5 @@
-"""ctypes binding of libmtad.so: the same entry points as include/mtad.h, argument marshalling only.
+"""ctypes binding of libmtad.so: the same entry points as include/mtad.h, argument marshalling only (the operators that need no
+context have their tensor form in ops.py).
 
 Every step of the verification path runs inside the library's CUDA kernels; this module only turns torch
 tensors into pointers.  There is no fallback: if the library is missing or cannot be loaded, importing a
@@ -35,6 +36,40 @@ class ModelDesc(C.Structure):
 class Result(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("eta", "winner", "path", "n_out", "out_tok", "out_lp", "node_lp",
                                            "node_LP", "row_lse", "row_cand", "row_cand_lp", "margin", "status")]
+
+
+class PagedKV(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("table", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64), ("table_stride", C.c_int64),
+                ("dtype", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PagedRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("lens", "n_rows", "pos", "q", "k", "v", "q_out", "status")] + \
+               [(n, C.c_int64) for n in ("q_stride_seq", "q_stride_row", "q_stride_head", "kv_stride_seq", "kv_stride_row",
+                                         "kv_stride_head", "out_stride_seq", "out_stride_row", "out_stride_head")] + \
+               [(n, C.c_int32) for n in ("dtype", "batch", "rows", "n_q_heads")] + [("rope_base", C.c_float)]
+
+
+class PagedAttn(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("lens", "n_rows", "q", "out", "lse", "weights", "status")] + \
+               [(n, C.c_int64) for n in ("q_stride_seq", "q_stride_row", "q_stride_head", "out_stride_seq", "out_stride_row",
+                                         "out_stride_head", "weights_stride_seq", "weights_stride_head")] + \
+               [(n, C.c_int32) for n in ("batch", "rows", "n_q_heads", "window", "sinks", "max_len")] + [("scale", C.c_float)]
+
+
+class PagedEviction(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("lens", "scores", "kept", "new_lens", "scores_out", "status")] + \
+               [(n, C.c_int64) for n in ("scores_stride_seq", "scores_stride_head", "out_stride_seq", "out_stride_head")] + \
+               [(n, C.c_int32) for n in ("batch", "max_len", "keep", "first", "recent")]
+
+
+class AcceptRows(C.Structure):
+    _fields_ = [("logits", C.c_void_p)] + \
+               [(n, C.c_int64) for n in ("logits_stride_seq", "logits_stride_row", "draft_stride_seq", "draft_stride_row")] + \
+               [(n, C.c_void_p) for n in ("draft_tok", "n_draft", "last_uniform")] + \
+               [(n, C.c_int32) for n in ("dtype", "batch", "gamma", "vocab")] + [("temperature", C.c_float), ("draft_temperature", C.c_float)]
 
 
 class Extent(C.Structure):
@@ -97,6 +132,13 @@ def load_library() -> C.CDLL:
     lib.mtad_kernel_launches.argtypes = []
     lib.mtad_debug_gemm.argtypes = [P, P, I, I, P, I, P, I, P]
     lib.mtad_verify_chain_static.argtypes = [MD, C.c_int32, C.c_int32, I, P, P, F, P, RS, P]
+    KV = C.POINTER(PagedKV)
+    lib.mtad_paged_append.argtypes = [KV, C.POINTER(PagedRows), P]
+    lib.mtad_paged_attention_workspace.argtypes = [KV, C.POINTER(PagedAttn), C.POINTER(C.c_size_t)]
+    lib.mtad_paged_attention.argtypes = [KV, C.POINTER(PagedAttn), P, C.c_size_t, P]
+    lib.mtad_paged_evict.argtypes = [KV, C.POINTER(PagedEviction), P]
+    lib.mtad_accept_chain.argtypes = [C.POINTER(AcceptRows), P, F, RS, P]
+    lib.mtad_accept_chain_spd.argtypes = [C.POINTER(AcceptRows), P, P, RS, P]
     for n in EXPORTS:
         if n not in ("mtad_status_str", "mtad_kernel_launches"):
             getattr(lib, n).restype = I

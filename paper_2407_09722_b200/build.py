@@ -1,4 +1,4 @@
-"""Compile the CUDA sources into libmtad.so (sm_100a only) next to this file.
+"""Compile the CUDA sources into libmtad.so (sm_100a only) next to this file, and the tensor form of its operators into _ops.so.
 
     python -m paper_2407_09722_b200.build [--verbose]
 """
@@ -7,37 +7,53 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmtad.so")
+OPS = os.path.join(HERE, "_ops.so")
+OPS_SRC = os.path.join(CSRC, "ops_py.cpp")
+HEADER = os.path.join(ROOT, "include", "mtad.h")
 
 
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "mtad.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+def _stale(target: str, deps) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
-        return LIB
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", LIB] + os.environ.get("MTAD_NVCC_FLAGS", "").split() + sources()
+    if force or _stale(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [HEADER]):
+        nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+        cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-t", "0",
+               "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+               "-o", LIB] + os.environ.get("MTAD_NVCC_FLAGS", "").split() + sources()
+        if verbose:
+            cmd.insert(1, "-Xptxas=-v")
+            print(" ".join(cmd))
+        subprocess.run(cmd, check=True)
+    if force or _stale(OPS, [OPS_SRC, HEADER]):
+        build_ops(verbose)
+    return LIB
+
+
+def build_ops(verbose: bool = False) -> str:
+    import torch
+    t = os.path.dirname(os.path.abspath(torch.__file__))
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    for d in (os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+              sysconfig.get_paths()["include"], "/usr/local/cuda/include"):
+        cmd += ["-I", d]
+    cmd += [OPS_SRC, "-o", OPS, "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
+            "-L", HERE, "-l:libmtad.so", "-Wl,-rpath,$ORIGIN"]
     if verbose:
-        cmd.insert(1, "-Xptxas=-v")
         print(" ".join(cmd))
     subprocess.run(cmd, check=True)
-    return LIB
+    return OPS
 
 
 if __name__ == "__main__":

@@ -77,6 +77,8 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const AppendArgs a, 
     const int half = a.kv.hd >> 1;
     __shared__ float s_cos[MTAD_PAGED_MAX_HEAD_DIM / 2], s_sin[MTAD_PAGED_MAX_HEAD_DIM / 2];
     __shared__ long long s_off;
+    pdl_wait();
+    pdl_trigger();
     const int len = __ldg(a.lens + b), nb = a.n_rows ? min(max(__ldg(a.n_rows + b), 0), a.R) : a.R;
     if (r >= nb) return;
     const long long slot = (long long)len - nb + r;
@@ -132,10 +134,9 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const AppendArgs a, 
 template <typename Src, typename T>
 cudaError_t launch_append(const AppendArgs& a, const RopeTable& rope, int B, cudaStream_t st) {
     const dim3 grid(B * a.R, a.shares);
-    if (a.kv.hd % 16 == 0) append_kernel<Src, T, 8><<<grid, AP_THREADS, 0, st>>>(a, rope);
-    else append_kernel<Src, T, 4><<<grid, AP_THREADS, 0, st>>>(a, rope);
     mtad_ops_count(1);
-    return cudaGetLastError();
+    return a.kv.hd % 16 == 0 ? launch_pdl(append_kernel<Src, T, 8>, grid, dim3(AP_THREADS), 0, st, true, a, rope)
+                             : launch_pdl(append_kernel<Src, T, 4>, grid, dim3(AP_THREADS), 0, st, true, a, rope);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -513,8 +514,13 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* c, void* s
     const int V = kv->head_dim % 16 == 0 ? 8 : 4, half = kv->head_dim / 2;
     a.nv = fast_div((uint32_t)(half / V));
     a.nv2 = fast_div((uint32_t)(kv->head_dim / V));
-    RopeTable rope;
-    for (int i = 0; i < half && a.rope; ++i) rope.v[i] = exp2(-(2.0 * i / kv->head_dim) * log2((double)c->rope_base));
+    // (frequencies of this thread's last base and head size: a hundred exponentials would take as long as the launch)
+    static thread_local struct { float base; int hd; RopeTable t; } rope{0.f, 0, {}};
+    if (a.rope && (rope.base != c->rope_base || rope.hd != kv->head_dim)) {
+        for (int i = 0; i < half; ++i) rope.t.v[i] = exp2(-(2.0 * i / kv->head_dim) * log2((double)c->rope_base));
+        rope.base = c->rope_base;
+        rope.hd = kv->head_dim;
+    }
     // few rows: their heads are shared out until every SM has two blocks
     const int all = (a.Hq + a.kv.Hkv) * (half / V) + a.kv.Hkv * (kv->head_dim / V);
     const int most = (all + AP_THREADS - 1) / AP_THREADS, want = (296 + c->batch * c->rows - 1) / (c->batch * c->rows);
@@ -522,11 +528,11 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* c, void* s
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (kv->dtype == MTAD_BF16)
-        e = c->dtype == MTAD_F32 ? launch_append<float, __nv_bfloat16>(a, rope, c->batch, st)
-                                 : launch_append<__nv_bfloat16, __nv_bfloat16>(a, rope, c->batch, st);
+        e = c->dtype == MTAD_F32 ? launch_append<float, __nv_bfloat16>(a, rope.t, c->batch, st)
+                                 : launch_append<__nv_bfloat16, __nv_bfloat16>(a, rope.t, c->batch, st);
     else
-        e = c->dtype == MTAD_F32 ? launch_append<float, __half>(a, rope, c->batch, st)
-                                 : launch_append<__half, __half>(a, rope, c->batch, st);
+        e = c->dtype == MTAD_F32 ? launch_append<float, __half>(a, rope.t, c->batch, st)
+                                 : launch_append<__half, __half>(a, rope.t, c->batch, st);
     return ops_status(e);
 }
 

@@ -7,28 +7,20 @@ import torch
 
 import paper_2407_09722_b200 as M
 from paper_2407_09722_b200 import binding as Bn
-from paper_2407_09722_b200 import ops
 
 
 @pytest.fixture(scope="module")
 def lib():
     from paper_2407_09722_b200.build import build
     build()
-    lib, P, KV = M.load_library(), C.c_void_p, C.POINTER(ops.PagedKV)
-    lib.mtad_paged_append.argtypes = [KV, C.POINTER(ops.PagedRows), P]
-    lib.mtad_paged_attention_workspace.argtypes = [KV, C.POINTER(ops.PagedAttn), C.POINTER(C.c_size_t)]
-    lib.mtad_paged_attention.argtypes = [KV, C.POINTER(ops.PagedAttn), P, C.c_size_t, P]
-    lib.mtad_paged_evict.argtypes = [KV, C.POINTER(ops.PagedEviction), P]
-    lib.mtad_accept_chain.argtypes = [C.POINTER(ops.AcceptRows), P, C.c_float, C.POINTER(Bn.Result), P]
-    lib.mtad_accept_chain_spd.argtypes = [C.POINTER(ops.AcceptRows), P, P, C.POINTER(Bn.Result), P]
-    return lib
+    return M.load_library()
 
 
 def _kv(**kw):
     d = dict(k_pages=4096, v_pages=8192, table=256, page_stride=2 * 8 * 16 * 128, head_stride=16 * 128, slot_stride=128, table_stride=64,
              dtype=0, n_pages=100, page_size=16, n_kv_heads=8, head_dim=128, max_pages=64)
     d.update(kw)
-    return ops.PagedKV(**d)
+    return Bn.PagedKV(**d)
 
 
 BAD_KV = [(dict(k_pages=None), Bn.MTAD_E_INVALID), (dict(v_pages=8194), Bn.MTAD_E_INVALID), (dict(table=None), Bn.MTAD_E_INVALID),
@@ -43,7 +35,7 @@ def _attn(**kw):
     d = dict(lens=256, q=4096, out=8192, q_stride_seq=64 * 128, q_stride_row=64 * 128, q_stride_head=128, out_stride_seq=64 * 128,
              out_stride_row=64 * 128, out_stride_head=128, batch=2, rows=1, n_q_heads=64, max_len=1000, scale=0.0)
     d.update(kw)
-    return ops.PagedAttn(**d)
+    return Bn.PagedAttn(**d)
 
 
 def _rows(**kw):
@@ -51,14 +43,14 @@ def _rows(**kw):
              kv_stride_row=1024, kv_stride_head=128, out_stride_seq=8192, out_stride_row=8192, out_stride_head=128, dtype=0, batch=2, rows=1,
              n_q_heads=64, rope_base=10000.0)
     d.update(kw)
-    return ops.PagedRows(**d)
+    return Bn.PagedRows(**d)
 
 
 def _evict(**kw):
     d = dict(lens=256, scores=4096, kept=8192, new_lens=512, scores_stride_seq=8000, scores_stride_head=1000, batch=2, max_len=1000, keep=100,
              first=4, recent=10)
     d.update(kw)
-    return ops.PagedEviction(**d)
+    return Bn.PagedEviction(**d)
 
 
 @pytest.mark.parametrize("kw,code", BAD_KV)
@@ -85,16 +77,18 @@ def test_attention_refusals(lib, kw, code):
 
 def test_attention_workspace(lib):
     n = C.c_size_t(0)
-    assert lib.mtad_paged_attention_workspace(_kv(), _attn(), None) == Bn.MTAD_E_INVALID
-    assert lib.mtad_paged_attention_workspace(_kv(), None, C.byref(n)) == Bn.MTAD_E_INVALID
-    assert lib.mtad_paged_attention_workspace(_kv(), _attn(), C.byref(n)) == 0
+    kv = _kv(max_pages=4096, table_stride=4096)
+    assert lib.mtad_paged_attention_workspace(kv, _attn(), None) == Bn.MTAD_E_INVALID
+    assert lib.mtad_paged_attention_workspace(kv, None, C.byref(n)) == Bn.MTAD_E_INVALID
+    assert lib.mtad_paged_attention_workspace(kv, _attn(max_len=60000), C.byref(n)) == 0
     need = n.value
     assert need > 0 and need % 256 == 0
     for ws, size in ((None, need), (4096, need - 1), (4100, need)):
-        assert lib.mtad_paged_attention(_kv(), _attn(), ws, size, None) == Bn.MTAD_E_WORKSPACE
-    assert lib.mtad_paged_attention_workspace(_kv(), _attn(weights=256, weights_stride_seq=8000, weights_stride_head=1000), C.byref(n)) == 0
+        assert lib.mtad_paged_attention(kv, _attn(max_len=60000), ws, size, None) == Bn.MTAD_E_WORKSPACE
+    more = dict(max_len=60000, weights=256, weights_stride_seq=480000, weights_stride_head=60000)
+    assert lib.mtad_paged_attention_workspace(kv, _attn(**more), C.byref(n)) == 0
     assert n.value > need
-    assert lib.mtad_paged_attention_workspace(_kv(), _attn(max_len=200), C.byref(n)) == 0 and n.value == 0      # a block takes a head whole
+    assert lib.mtad_paged_attention_workspace(kv, _attn(max_len=200), C.byref(n)) == 0 and n.value == 0         # a cluster has a head
     # an hour of tiles more than a launch can count
     big = _kv(page_size=1 << 20, max_pages=1000, table_stride=1000)
     assert lib.mtad_paged_attention_workspace(big, _attn(max_len=1000 << 20, batch=4096), C.byref(n)) == Bn.MTAD_E_CAPACITY
@@ -134,7 +128,7 @@ def _accept(**kw):
     d = dict(logits=4096, logits_stride_seq=5000, logits_stride_row=1000, draft_stride_seq=4000, draft_stride_row=1000, draft_tok=256,
              last_uniform=512, dtype=2, batch=2, gamma=4, vocab=1000, temperature=1.0, draft_temperature=1.0)
     d.update(kw)
-    return ops.AcceptRows(**d)
+    return Bn.AcceptRows(**d)
 
 
 def _result(**kw):
