@@ -248,9 +248,9 @@ template <typename T, int HD, int ROWS> struct Narrow {
             }
     }
     __device__ __forceinline__ void tile(const AttnArgs& a, const TileAt& t, uint32_t, float* scores, int chunks) {
-        float s[N8][4];              // (key g | g + 8, row 2t | 2t + 1)
+        float s[N8][4], s2[N8][4];   // (key g | g + 8, row 2t | 2t + 1), in two sums whose products do not wait for one another
 #pragma unroll
-        for (int n = 0; n < N8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        for (int n = 0; n < N8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = s2[n][0] = s2[n][1] = s2[n][2] = s2[n][3] = 0.f;
         const uint32_t at_k = t.k + at<HD>(lane & 15, lane >> 4);
         const uint32_t at_v = t.v + at<HD>((lane >> 4) * 8 + (lane & 7), (lane >> 3) & 1);
 #pragma unroll
@@ -258,8 +258,12 @@ template <typename T, int HD, int ROWS> struct Narrow {
             uint32_t ka[4];
             ldsm4(ka, at_k ^ (k << 5));
 #pragma unroll
-            for (int n = 0; n < N8; ++n) mma<T>(s[n], ka, q[k][n][0], q[k][n][1]);
+            for (int n = 0; n < N8; ++n) mma<T>((k & 1) ? s2[n] : s[n], ka, q[k][n][0], q[k][n][1]);
         }
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] += s2[n][e];
         bool raise = false;
 #pragma unroll
         for (int n = 0; n < N8; ++n) {
@@ -340,14 +344,18 @@ template <typename T, int HD, int ROWS> struct Narrow {
                 ph[n][half] = transposed(hi);
                 pl[n][half] = transposed(Num<T>::pack(u - x.x, v - x.y));
             }
+        constexpr int STEP = HD / 16 < 8 ? HD / 16 : 8;   // columns' products in flight
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) {
-            uint32_t va[4];
-            ldsm4t(va, at_v ^ (d << 5));
+        for (int d0 = 0; d0 < HD / 16; d0 += STEP) {
+            uint32_t va[STEP][4];
+#pragma unroll
+            for (int d = 0; d < STEP; ++d) ldsm4t(va[d], at_v ^ ((d0 + d) << 5));
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
-                mma<T>(o[d][n], va, ph[n][0], ph[n][1]);
-                mma<T>(o[d][n], va, pl[n][0], pl[n][1]);
+#pragma unroll
+                for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], ph[n][0], ph[n][1]);
+#pragma unroll
+                for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], pl[n][0], pl[n][1]);
             }
         }
     }
