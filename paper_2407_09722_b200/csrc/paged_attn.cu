@@ -178,12 +178,13 @@ __device__ __forceinline__ bool mixed(const AttnArgs& a, const TileAt& t, int j)
 // whether one of the 16 value rows at `first` that only some rows see holds an infinity or a NaN (per lane)
 template <typename T, int HD>
 __device__ __forceinline__ bool odd_value(const AttnArgs& a, const TileAt& t, int first, int chunks, int lane) {
-    bool odd = false;
-    if (lane < 16 && mixed(a, t, t.j0 + first + lane))
-        for (int c = 0; c < chunks; ++c) {
+    bool odd = false;                                     // (a lane has every other piece of a row)
+    if (mixed(a, t, t.j0 + first + (lane & 15)))
+#pragma unroll 4
+        for (int c = lane >> 4; c < chunks; c += 2) {
             uint32_t w[4];
             asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                         : "r"(t.v + at<HD>(first + lane, c)));
+                         : "r"(t.v + at<HD>(first + (lane & 15), c)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd = odd || (w[e] & Num<T>::kExp) == Num<T>::kExp || ((w[e] >> 16) & Num<T>::kExp) == Num<T>::kExp;
         }
@@ -670,6 +671,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
     __shared__ float2 s_part[KW * ROWS];
     __shared__ float2 s_ml[ROWS];                         // the block's; read by the cluster
     __shared__ float2 s_all[LIST ? 1 : MAX_CLUSTER][LIST ? 1 : ROWS];
+    __shared__ float4 s_x[LIST || KW == 1 ? 1 : NT / 32][LIST || KW == 1 ? 1 : 32];
     __shared__ long long s_scan[4];
     __shared__ long long s_first[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -690,8 +692,9 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         P.hr = head - P.b * HR;
         P.s = seq_of<TK>(a, P.b);
         if (P.s.nt == 0) return;                          // (the whole cluster)
-        P.t = (int)((long long)P.s.nt * rank / a.cluster);
-        count = (int)((long long)P.s.nt * (rank + 1) / a.cluster) - P.t;
+        // (the last block, whose last tile takes the longest, has none of the odd ones)
+        P.t = (int)(((long long)P.s.nt * rank + a.cluster - 1) / a.cluster);
+        count = (int)(((long long)P.s.nt * (rank + 1) + a.cluster - 1) / a.cluster) - P.t;
     } else {
         // first tiles of the sequences: up to 32 by one warp (every warp for itself), more by the block
         const int lanes = a.B <= 32 ? 32 : NT, me = a.B <= 32 ? lane : tid;
@@ -774,17 +777,23 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         copy_rows<HD>(a, spot, c.b, (long long)(c.hr / a.RB) * a.kv.head_stride, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks);
     };
     int ahead = 0;                                        // tiles handed to the copies
-    Spot spot{-1, 0};
-    if (count > 0) spot = find(P);
+    Spot spot{-1, 0}, begin[S - 1];
+    Cursor from[S - 1];
     read_q();
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        if (ahead < count) {
-            copy(spot, P, s);
-            if (++ahead < count) { advance<TK>(a, P); spot = find(P); }
+    for (int s = 0; s < S - 1; ++s)                       // (the first tiles' pages are asked for together)
+        if (s < count) {
+            begin[s] = find(P);
+            from[s] = P;
+            if (s + 1 < count) advance<TK>(a, P);
         }
+    if (S - 1 < count) spot = find(P);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) {
+        if (s < count) copy(begin[s], from[s], s);
         cp_commit();
     }
+    ahead = min(S - 1, count);
     put_q();
 
     int stage = 0;
@@ -881,31 +890,47 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
             s_all[k][m] = CS > 1 ? *cluster.map_shared_rank(&s_ml[m], k) : s_ml[m];
         }
         __syncthreads();
-        // ---- a block adds the cluster's outputs of its share of (row, four columns)
-        const int h = C.hr / a.RB, per_row = a.kv.hd / 4, valid = max(rows, 0) * per_row;
-        for (int i = rank * NT + tid; i < valid; i += CS * NT) {
-            const int m = i / per_row, d = (i - m * per_row) * 4;
+        // ---- a block adds the cluster's outputs of its share of (row, four columns): a warp per output of a warp, neighbouring columns by
+        // neighbouring lanes (requests to another block's memory that are not whole lines take ten times as long)
+        const int h = C.hr / a.RB, per_row = a.kv.hd / 4, valid = max(rows, 0) * per_row, w = warp % KW;
+        for (int i0 = rank * (32 * L::MT); i0 < valid; i0 += CS * (32 * L::MT)) {
+            const int i = i0 + warp / KW * 32 + lane, m = min(i, valid - 1) / per_row, d = (min(i, valid - 1) - m * per_row) * 4;
+            float4 x[MAX_CLUSTER];
+#pragma unroll
+            for (int k = 0; k < MAX_CLUSTER; ++k)
+                if (k < CS) x[k] = *reinterpret_cast<const float4*>((CS > 1 ? cluster.map_shared_rank(part, k) : part) + (w * ROWS + m) * L::LDO + d);
             float mx = s_all[0][m].x, sum = 0.f;
             for (int k = 1; k < CS; ++k) mx = fmaxf(mx, s_all[k][m].x);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int k = 0; k < CS; ++k) {
-                const float2 ml = s_all[k][m];
-                const float f = ml.x == mx ? 1.f : ex2(ml.x - mx);
-                sum += f * ml.y;
-                const float* src = CS > 1 ? cluster.map_shared_rank(part, k) : part;
 #pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    const float4 x = *reinterpret_cast<const float4*>(src + (w * ROWS + m) * L::LDO + d);
-                    acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
+            for (int k = 0; k < MAX_CLUSTER; ++k)
+                if (k < CS) {
+                    const float2 ml = s_all[k][m];
+                    const float f = ml.x == mx ? 1.f : ex2(ml.x - mx);
+                    sum += f * ml.y;
+                    acc.x += f * x[k].x; acc.y += f * x[k].y; acc.z += f * x[k].z; acc.w += f * x[k].w;
                 }
+            if constexpr (KW > 1) {
+                s_x[warp][lane] = acc;
+                __syncthreads();
+                if (w == 0)
+#pragma unroll
+                    for (int k = 1; k < KW; ++k) {
+                        const float4 y = s_x[warp + k][lane];
+                        acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
+                    }
             }
-            const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-            const float inv = inverse(sum);
-            *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
-                make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
-            if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
+            if (w == 0 && i < valid) {
+                const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
+                const float inv = inverse(sum);
+                *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
+                    make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
+                if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
+            }
+            if constexpr (KW > 1) __syncthreads();
         }
+        // (no block leaves while another reads its shared memory)
+        if (CS > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         // ---- weights of the slots of this block's tiles, from the scores that it wrote itself (one row block a head: see make_plan)
         if (a.weights) {
             float* const s_lse = reinterpret_cast<float*>(s_part);
@@ -930,7 +955,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
                 dst[j] += acc;
             }
         }
-        if (CS > 1) cluster.sync();                       // (no block leaves while another reads its shared memory)
+        if (CS > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
 }
 
@@ -1012,16 +1037,23 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
         copy_rows<HD>(a, spot, c.b, c.hr * a.kv.head_stride, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks);
     };
     int ahead = 0;
-    Spot spot = find(P);
+    Spot spot{-1, 0}, begin[S - 1];
+    Cursor from[S - 1];
     read_q();
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        if (ahead < count) {
-            copy(spot, P, s);
-            if (++ahead < count) { advance<RW>(a, P); spot = find(P); }
+    for (int s = 0; s < S - 1; ++s)                       // (the first tiles' pages are asked for together)
+        if (s < count) {
+            begin[s] = find(P);
+            from[s] = P;
+            if (s + 1 < count) advance<RW>(a, P);
         }
+    if (S - 1 < count) spot = find(P);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) {
+        if (s < count) copy(begin[s], from[s], s);
         cp_commit();
     }
+    ahead = min(S - 1, count);
     put_q();
     int stage = 0, first_t = C.t;
     for (int i = 0; i < count; ++i) {
