@@ -55,7 +55,7 @@ struct AttnArgs {
     int cluster;                     // blocks of a head; 0: the list is cut evenly over the grid
     int grid;
     // workspace
-    long long* plan;                 // [0] tiles of a block, [1 .. B + 1] first tile of every sequence
+    int* plan;                       // [0] tiles of a block, [1 .. B + 1] first tile of every sequence
     float* part_o;                   // [2 * grid][rows_block][HD]
     float2* part_ml;                 // [2 * grid][rows_block] maximum (log2 domain) and sum
     float* row_lse2;                 // [B][Hkv * RB][rows_block] log2 of the sums of heads that one block saw whole, only with weights
@@ -150,7 +150,7 @@ template <int HD, int ROWS> struct Tile {
     static constexpr int CH = HD / 8;                    // 16-byte pieces of a row
     static constexpr int BYTES = TK * HD * 2;            // keys (or values) of a tile
     // two blocks on an SM (one with heads of 256): 70 to 105 KB of a block's shared memory on their way or in use
-    static constexpr int STAGES = HD == 64 ? (ROWS <= 16 ? 6 : 4) : (ROWS <= 16 ? 3 : 2);
+    static constexpr int STAGES = HD == 64 ? 4 : ROWS <= 16 ? 3 : 2;
     static constexpr int BLOCKS = HD == 256 ? 1 : 2;
     static constexpr int MT = ROWS <= 16 ? 1 : ROWS / 16;                // warps over the rows; 4 / MT over the keys of a tile
     static constexpr int Q = ROWS <= 16 ? 0 : ROWS * HD * 2;
@@ -672,8 +672,8 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
     __shared__ float2 s_ml[ROWS];                         // the block's; read by the cluster
     __shared__ float2 s_all[LIST ? 1 : MAX_CLUSTER][LIST ? 1 : ROWS];
     __shared__ float4 s_x[LIST || KW == 1 ? 1 : NT / 32][LIST || KW == 1 ? 1 : 32];
-    __shared__ long long s_scan[4];
-    __shared__ long long s_first[2];
+    __shared__ int s_scan[4];
+    __shared__ int s_first[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t sm = (uint32_t)__cvta_generic_to_shared(smem);
     const uint32_t sm_q = sm + S * 2 * L::BYTES;
@@ -699,15 +699,15 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         // first tiles of the sequences: up to 32 by one warp (every warp for itself), more by the block
         const int lanes = a.B <= 32 ? 32 : NT, me = a.B <= 32 ? lane : tid;
         const int each = (a.B + lanes - 1) / lanes, b0 = min(me * each, a.B), b1 = min(b0 + each, a.B);
-        long long mine = 0;
-        for (int b = b0; b < b1; ++b) mine += (long long)seq_of<TK>(a, b).nt * HR;
-        long long incl = mine;
+        int mine = 0;
+        for (int b = b0; b < b1; ++b) mine += seq_of<TK>(a, b).nt * HR;
+        int incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += x;
         }
-        long long total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine;
+        int total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine;
         if (a.B > 32) {
             if (lane == 31) s_scan[warp] = incl;
             __syncthreads();
@@ -718,20 +718,23 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
                 total += s_scan[w];
             }
         }
-        const long long per = (total + a.grid - 1) / a.grid, start = per * blockIdx.x, end = min(total, start + per);
+        const int per = (int)(((unsigned)total + a.grid - 1) / (unsigned)a.grid);
+        const long long first = (long long)per * blockIdx.x;
+        if (blockIdx.x != 0 && first >= total) return;
+        const int start = (int)first, end = min(total, start + min(per, total - start));
         if (blockIdx.x == 0 && (a.B > 32 || warp == 0)) { // for the second kernel
             if (me == 0) { a.plan[0] = per; a.plan[a.B + 1] = total; }
-            long long x = base;
-            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += (long long)seq_of<TK>(a, b).nt * HR; }
+            int x = base;
+            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += seq_of<TK>(a, b).nt * HR; }
         }
         if (start >= end) return;
-        count = (int)(end - start);
-        long long in = 0;
+        count = end - start;
+        int in = 0;
         const bool here = start >= base && start < base + mine;
         int b = b0;
         if (here)
             for (in = start - base;; ++b) {
-                const long long n = (long long)seq_of<TK>(a, b).nt * HR;
+                const int n = seq_of<TK>(a, b).nt * HR;
                 if (in < n) break;
                 in -= n;
             }
@@ -742,13 +745,13 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         } else {
             if (here) { s_first[0] = b; s_first[1] = in; }
             __syncthreads();
-            b = (int)s_first[0];
+            b = s_first[0];
             in = s_first[1];
         }
         P.b = b;
         P.s = seq_of<TK>(a, b);
-        P.hr = (int)(in / P.s.nt);
-        P.t = (int)(in - (long long)P.hr * P.s.nt);
+        P.hr = in / P.s.nt;
+        P.t = in - P.hr * P.s.nt;
     }
     Cursor C = P;
     Core core;
@@ -982,29 +985,29 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
     Cursor P;
     {
         const int each = (a.B + 31) / 32, b0 = min(lane * each, a.B), b1 = min(b0 + each, a.B);
-        long long mine = 0;
-        for (int b = b0; b < b1; ++b) mine += (long long)seq_of<RW>(a, b).nt * Hkv;
-        long long incl = mine;
+        int mine = 0;
+        for (int b = b0; b < b1; ++b) mine += seq_of<RW>(a, b).nt * Hkv;
+        int incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += x;
         }
-        const long long total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine, per = (total + a.grid - 1) / a.grid;
+        const int total = __shfl_sync(0xffffffffu, incl, 31), base = incl - mine, per = (int)(((unsigned)total + a.grid - 1) / (unsigned)a.grid);
         if (worker == 0) {                                // for the second kernel
             if (lane == 0) a.plan[0] = per;
-            long long x = base;
-            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += (long long)seq_of<RW>(a, b).nt * Hkv; }
+            int x = base;
+            for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += seq_of<RW>(a, b).nt * Hkv; }
         }
-        const long long start = per * worker;
-        if (start >= total) return;
-        count = (int)min(per, total - start);
+        if ((long long)per * worker >= total) return;
+        const int start = per * worker;
+        count = min(per, total - start);
         const bool here = start >= base && start < base + mine;
         int b = b0;
-        long long in = start - base;
+        int in = start - base;
         if (here)
             for (;; ++b) {
-                const long long n = (long long)seq_of<RW>(a, b).nt * Hkv;
+                const int n = seq_of<RW>(a, b).nt * Hkv;
                 if (in < n) break;
                 in -= n;
             }
@@ -1012,8 +1015,8 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
         P.b = __shfl_sync(0xffffffffu, b, from);
         in = __shfl_sync(0xffffffffu, in, from);
         P.s = seq_of<RW>(a, P.b);
-        P.hr = (int)(in / P.s.nt);
-        P.t = (int)(in - (long long)P.hr * P.s.nt);
+        P.hr = in / P.s.nt;
+        P.t = in - P.hr * P.s.nt;
     }
     Cursor C = P;
     Core core;
@@ -1125,19 +1128,18 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
 // ---- what the blocks left of heads that were cut, and the weights
 
 struct Pieces {                      // the shares that hold a head's tiles
-    long long per, s, c0;
-    int n;
+    int per, s, c0, n;
 };
 __device__ __forceinline__ Pieces pieces_of(const AttnArgs& a, const Seq& q, int b, int hr) {
     Pieces p;
     p.per = a.plan[0];
-    p.s = a.plan[1 + b] + (long long)hr * q.nt;
+    p.s = a.plan[1 + b] + hr * q.nt;
     p.c0 = p.s / p.per;
-    p.n = (int)((p.s + q.nt - 1) / p.per - p.c0) + 1;
+    p.n = (p.s + q.nt - 1) / p.per - p.c0 + 1;
     return p;
 }
 __device__ __forceinline__ long long place_of(const Pieces& p, int i) {
-    return 2 * (p.c0 + i) + (i == 0 && p.s > p.c0 * p.per ? 1 : 0);
+    return 2ll * (p.c0 + i) + (i == 0 && p.s > p.c0 * p.per ? 1 : 0);
 }
 // largest maximum and the sum relative to it of row m, over the pieces (a warp)
 __device__ __forceinline__ float2 joined(const AttnArgs& a, const Pieces& p, int m, int lane) {
@@ -1158,8 +1160,8 @@ constexpr int W_KEYS = 512;          // slots of a block that adds weights
 
 // Blocks [0, n_join): a warp per query row adds the pieces of its output.  Blocks beyond: the weights of W_KEYS slots of a KV head,
 // exp(score - lse) summed over the rows and the heads of the group and added to what is there.
-template <typename T, int HD, int UNIT>
-__global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, int groups) {
+template <typename T, int HD, int UNIT, bool WEIGHTS>
+__global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_join, int groups) {
     constexpr int PER = HD / 32;     // columns of a lane
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, HR = a.kv.Hkv * a.RB;
     __shared__ float s_lse[MAX_ROWS_BLOCK];
@@ -1197,27 +1199,41 @@ __global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, 
         if (a.lse && lane == 0) a.lse[((long long)b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (ml.x + log2f(ml.y)) * LN2;
         return;
     }
+    if constexpr (!WEIGHTS) return;
     const int per_head = (a.max_len + W_KEYS - 1) / W_KEYS, w = blockIdx.x - n_join, bh = w / per_head, b = bh / a.kv.Hkv, h = bh - b * a.kv.Hkv;
     const int k0 = (w - bh * per_head) * W_KEYS;
     const Seq q = seq_of<UNIT>(a, b);
     if (q.nt == 0 || k0 >= q.len) return;
-    // slots of tiles that no row sees have no scores
-    bool there[4];
-    float acc[4];
+    const int j = k0 + tid * 4;                           // (four neighbouring slots lie in one tile; tiles that no row sees have no scores)
+    const bool there = j < q.len && (j / UNIT < q.ns || j / UNIT >= q.ns + q.skip);
+    if (!__syncthreads_or(there)) return;
+    const int RBL = a.rows_block;
+    float* const dst = a.weights + (long long)b * a.w_sb + (long long)h * a.w_sh + j;
+    // everything that does not need the sums is asked for before they are known
+    float old[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int j = k0 + k * NT + tid, t = j / UNIT;
-        there[k] = j < q.len && (t < q.ns || t >= q.ns + q.skip);
-        acc[k] = 0.f;
-    }
-    if (!__syncthreads_or(there[0] || there[1] || there[2] || there[3])) return;
+    for (int k = 0; k < 4; ++k) old[k] = there && j + k < q.len ? dst[k] : 0.f;
     for (int rb = 0; rb < a.RB; ++rb) {
-        const int hr = h * a.RB + rb, rows = min(q.nb * a.G - rb * a.rows_block, a.rows_block);
+        const int hr = h * a.RB + rb, rows = min(q.nb * a.G - rb * RBL, RBL);
         if (rows <= 0) break;
+        const float* z = a.scores + ((long long)bh * (a.RB * RBL) + rb * RBL) * a.score_ld + j;
+        float4 x[8];
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+            if (there && m < rows) x[m] = *reinterpret_cast<const float4*>(z + m * a.score_ld);
         const Pieces p = pieces_of(a, q, b, hr);
         __syncthreads();
         if (p.n == 1) {
-            if (tid < rows) s_lse[tid] = a.row_lse2[((long long)b * HR + hr) * a.rows_block + tid];
+            if (tid < rows) s_lse[tid] = a.row_lse2[((long long)b * HR + hr) * RBL + tid];
+        } else if (p.n <= 4 && rows <= 32) {              // (four lanes a row)
+            const int m = tid >> 2, i = tid & 3;
+            const float2 ml = m < rows && i < p.n ? a.part_ml[place_of(p, i) * RBL + m] : make_float2(-CUDART_INF_F, 0.f);
+            float mx = fmaxf(ml.x, __shfl_xor_sync(0xffffffffu, ml.x, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            float sum = ml.y * (ml.x == mx ? 1.f : ex2(ml.x - mx));
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            if (m < rows && i == 0) s_lse[m] = mx + log2f(sum);
         } else {
             for (int m = warp; m < rows; m += 4) {
                 const float2 ml = joined(a, p, m, lane);
@@ -1225,20 +1241,22 @@ __global__ void __launch_bounds__(NT) join_kernel(const AttnArgs a, int n_join, 
             }
         }
         __syncthreads();
-        const float* z = a.scores + ((long long)bh * (a.RB * a.rows_block) + rb * a.rows_block) * a.score_ld + k0 + tid;
-#pragma unroll 4
-        for (int m = 0; m < rows; ++m) {
-            const float lse = s_lse[m];
-            if (lse == -CUDART_INF_F) continue;           // (a row that sees nothing)
+        for (int m0 = 0; m0 < rows; m0 += 8) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (there[k]) acc[k] += ex2(z[(long long)m * a.score_ld + k * NT] - lse);
+            for (int m = 0; m < 8; ++m) {
+                if (m0 + m >= rows) break;
+                const float lse = s_lse[m0 + m];
+                if (lse == -CUDART_INF_F) continue;       // (a row that sees nothing has no scores)
+                acc[0] += ex2(x[m].x - lse); acc[1] += ex2(x[m].y - lse); acc[2] += ex2(x[m].z - lse); acc[3] += ex2(x[m].w - lse);
+            }
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                if (there && m0 + 8 + m < rows) x[m] = *reinterpret_cast<const float4*>(z + (m0 + 8 + m) * a.score_ld);
         }
     }
-    float* dst = a.weights + (long long)b * a.w_sb + (long long)h * a.w_sh + k0 + tid;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        if (there[k]) dst[k * NT] += acc[k];
+        if (there && j + k < q.len) dst[k] = old[k] + acc[k];
 }
 
 // ---- host
@@ -1310,7 +1328,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     p->grid = (int)(list ? std::min(heads * tiles, fill) : heads * cs);
     a.grid = p->narrow ? p->grid * (NT / 32) : p->grid;  // shares
     Carve w;
-    p->plan = w.take(list ? sizeof(long long) * (a.B + 2) : 0);
+    p->plan = w.take(list ? sizeof(int) * (a.B + 2) : 0);
     p->part_o = w.take(list ? sizeof(float) * 2 * (size_t)a.grid * a.rows_block * p->HD : 0);
     p->part_ml = w.take(list ? sizeof(float2) * 2 * (size_t)a.grid * a.rows_block : 0);
     a.score_ld = a.weights ? (long long)((a.max_len + TK - 1) / TK) * TK : 0;
@@ -1365,8 +1383,9 @@ cudaError_t launch_hd(const AttnPlan& p, cudaStream_t st) {
     const int groups = (std::min(p.a.R * p.a.G, p.a.rows_block) + 3) / 4;
     const int join = p.a.B * p.a.kv.Hkv * p.a.RB * groups;
     const int add = p.a.weights ? p.a.B * p.a.kv.Hkv * ((p.a.max_len + W_KEYS - 1) / W_KEYS) : 0;
-    return p.narrow ? launch_pdl(join_kernel<T, HD, RW>, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups)
-                    : launch_pdl(join_kernel<T, HD, TK>, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups);
+    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups); };
+    return p.narrow ? (add ? go(join_kernel<T, HD, RW, true>) : go(join_kernel<T, HD, RW, false>))
+                    : (add ? go(join_kernel<T, HD, TK, true>) : go(join_kernel<T, HD, TK, false>));
 }
 template <typename T>
 cudaError_t launch_t(const AttnPlan& p, cudaStream_t st) {
@@ -1395,7 +1414,7 @@ int mtad_paged_attention(const mtad_paged_kv* kv, const mtad_paged_attn* call, v
     if (rc != MTAD_OK) return rc;
     if (p.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes)) return MTAD_E_WORKSPACE;
     char* w = static_cast<char*>(workspace);
-    p.a.plan = reinterpret_cast<long long*>(w + p.plan);
+    p.a.plan = reinterpret_cast<int*>(w + p.plan);
     p.a.part_o = reinterpret_cast<float*>(w + p.part_o);
     p.a.part_ml = reinterpret_cast<float2*>(w + p.part_ml);
     p.a.row_lse2 = reinterpret_cast<float*>(w + p.row_lse2);
