@@ -346,7 +346,7 @@ typedef struct mtad_paged_kv {
     int32_t max_pages;                  /* entries of a table row */
 } mtad_paged_kv;
 
-/* New rows enter the cache.  Sequence b has n = n_rows[b] rows (rows where n_rows is NULL); row r goes to slot lens[b] - n + r: lens
+/* New rows enter the cache.  Sequence b has n = n_rows[b] rows (rows where n_rows is NULL; at most rows count); row r goes to slot lens[b] - n + r: lens
  * counts the slots after the call.  With rope_base >= 1 queries and keys are turned by the rotary embedding (half-split pairing (i, i +
  * head_dim/2), the angle reduced in 64 bits) at position pos[b] + r, or at the slot where pos is NULL; pos differs from the slot once
  * a cache has been thinned by mtad_paged_evict.  rope_base = 0: no rotation.  The arithmetic is fp32, rounded once to the cache's

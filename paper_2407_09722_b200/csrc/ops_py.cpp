@@ -50,6 +50,9 @@ int type_of(const Tensor& t) {
     }
 }
 
+// (a dimension of one entry may have any stride)
+int64_t step(const Tensor& t, int d) { return t.size(d) == 1 ? 0 : t.stride(d); }
+
 // The device of a call, and its stream: what is allocated here belongs to the stream that uses it
 struct On {
     c10::cuda::OptionalCUDAGuard device;
@@ -94,9 +97,9 @@ struct Pages {
         kv.k_pages = k.data_ptr();
         kv.v_pages = v.data_ptr();
         kv.table = static_cast<const int32_t*>(t.data_ptr());
-        kv.page_stride = k.stride(0);
-        kv.head_stride = k.stride(1);
-        kv.slot_stride = k.stride(2);
+        kv.page_stride = step(k, 0);
+        kv.head_stride = step(k, 1);
+        kv.slot_stride = k.size(2) == 1 ? k.size(3) : k.stride(2);
         kv.table_stride = std::max(t.stride(0), t.size(1));               // (of one row: whatever)
         kv.dtype = type_of(k);
         kv.n_pages = (int32_t)std::min<int64_t>(k.size(0), INT32_MAX);
@@ -146,8 +149,8 @@ PyObject* append(PyObject*, PyObject* const* x, Py_ssize_t n) {
         TORCH_CHECK_VALUE(out.scalar_type() == p.k.scalar_type() && out.size(2) == q.size(2), "q_out: the pages' type, q's heads");
         a.q = q.data_ptr();
         a.q_out = out.data_ptr();
-        a.q_stride_seq = q.stride(0); a.q_stride_row = q.stride(1); a.q_stride_head = q.stride(2);
-        a.out_stride_seq = out.stride(0); a.out_stride_row = out.stride(1); a.out_stride_head = out.stride(2);
+        a.q_stride_seq = step(q, 0); a.q_stride_row = step(q, 1); a.q_stride_head = step(q, 2);
+        a.out_stride_seq = step(out, 0); a.out_stride_row = step(out, 1); a.out_stride_head = step(out, 2);
         a.n_q_heads = (int32_t)std::min<int64_t>(q.size(2), INT32_MAX);
     }
     a.lens = as<int32_t>(plain(x[6], "lens", at::kInt, {b}, p.k));
@@ -156,7 +159,7 @@ PyObject* append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.status = as<uint32_t>(plain(x[11], "status", at::kInt, {b}, p.k));
     a.k = k.data_ptr();
     a.v = v.data_ptr();
-    a.kv_stride_seq = k.stride(0); a.kv_stride_row = k.stride(1); a.kv_stride_head = k.stride(2);
+    a.kv_stride_seq = step(k, 0); a.kv_stride_row = step(k, 1); a.kv_stride_head = step(k, 2);
     a.dtype = type_of(k);
     a.batch = (int32_t)std::min<int64_t>(b, INT32_MAX);
     a.rows = (int32_t)std::min<int64_t>(r, INT32_MAX);
@@ -203,8 +206,8 @@ PyObject* attention(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.status = as<uint32_t>(plain(x[14], "status", at::kInt, {b}, p.k));
     a.q = q.data_ptr();
     a.out = out.data_ptr();
-    a.q_stride_seq = q.stride(0); a.q_stride_row = q.stride(1); a.q_stride_head = q.stride(2);
-    a.out_stride_seq = out.stride(0); a.out_stride_row = out.stride(1); a.out_stride_head = out.stride(2);
+    a.q_stride_seq = step(q, 0); a.q_stride_row = step(q, 1); a.q_stride_head = step(q, 2);
+    a.out_stride_seq = step(out, 0); a.out_stride_row = step(out, 1); a.out_stride_head = step(out, 2);
     a.batch = (int32_t)std::min<int64_t>(b, INT32_MAX);
     a.rows = (int32_t)std::min<int64_t>(r, INT32_MAX);
     a.n_q_heads = (int32_t)std::min<int64_t>(hq, INT32_MAX);
