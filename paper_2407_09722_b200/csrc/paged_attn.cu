@@ -36,7 +36,7 @@ constexpr int TK = 64;               // keys of a tile
 constexpr int NT = 128;              // threads of a block
 constexpr int MAX_ROWS_BLOCK = 64;   // query rows (rows x heads of the group) of a block
 constexpr int MAX_CLUSTER = 8;
-constexpr int CLUSTER_TILES = 12;    // tiles of a block up to which a cluster has a head
+constexpr int CLUSTER_TILES = 12, CLUSTER_TILES_WIDE = 5;       // tiles of a block up to which a cluster has a head
 
 struct AttnArgs {
     PagedView kv;
@@ -671,7 +671,6 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
     __shared__ float2 s_part[KW * ROWS];
     __shared__ float2 s_ml[ROWS];                         // the block's; read by the cluster
     __shared__ float2 s_all[LIST ? 1 : MAX_CLUSTER][LIST ? 1 : ROWS];
-    __shared__ float4 s_x[LIST || KW == 1 ? 1 : NT / 32][LIST || KW == 1 ? 1 : 32];
     __shared__ int s_scan[4];
     __shared__ int s_first[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -886,22 +885,36 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         float* const part = reinterpret_cast<float*>(smem);               // [KW][ROWS][LDO]
         core.put(part + (warp / L::MT) * ROWS * L::LDO, L::LDO, 0, false);
         cg::cluster_group cluster = cg::this_cluster();
-        const int CS = a.cluster;
+        const int CS = a.cluster, per_row = a.kv.hd / 4, valid = max(rows, 0) * per_row, h = C.hr / a.RB;
+        __syncthreads();
+        if constexpr (KW > 1) {                           // the block's sum, over the first warp's
+#pragma unroll 2
+            for (int i = tid; i < valid; i += NT) {
+                const int m = i / per_row;
+                float4* at = reinterpret_cast<float4*>(part + m * L::LDO + (i - m * per_row) * 4);
+                float4 x[KW];
+#pragma unroll
+                for (int w = 0; w < KW; ++w) x[w] = at[w * (ROWS * L::LDO / 4)];
+#pragma unroll
+                for (int w = 1; w < KW; ++w) { x[0].x += x[w].x; x[0].y += x[w].y; x[0].z += x[w].z; x[0].w += x[w].w; }
+                *at = x[0];
+            }
+        }
         if (CS > 1) cluster.sync(); else __syncthreads();
         for (int i = tid; i < CS * ROWS; i += NT) {
             const int k = i / ROWS, m = i - k * ROWS;
             s_all[k][m] = CS > 1 ? *cluster.map_shared_rank(&s_ml[m], k) : s_ml[m];
         }
         __syncthreads();
-        // ---- a block adds the cluster's outputs of its share of (row, four columns): a warp per output of a warp, neighbouring columns by
-        // neighbouring lanes (requests to another block's memory that are not whole lines take ten times as long)
-        const int h = C.hr / a.RB, per_row = a.kv.hd / 4, valid = max(rows, 0) * per_row, w = warp % KW;
-        for (int i0 = rank * (32 * L::MT); i0 < valid; i0 += CS * (32 * L::MT)) {
-            const int i = i0 + warp / KW * 32 + lane, m = min(i, valid - 1) / per_row, d = (min(i, valid - 1) - m * per_row) * 4;
+        // ---- a block adds the cluster's sums of its share of (row, four columns), neighbouring columns by neighbouring lanes (requests to
+        // another block's memory that are not whole lines take ten times as long)
+        const int share = ((valid + CS - 1) / CS + 7) & ~7;
+        for (int i = rank * share + tid; i < min((rank + 1) * share, valid); i += NT) {
+            const int m = i / per_row, d = (i - m * per_row) * 4;
             float4 x[MAX_CLUSTER];
 #pragma unroll
             for (int k = 0; k < MAX_CLUSTER; ++k)
-                if (k < CS) x[k] = *reinterpret_cast<const float4*>((CS > 1 ? cluster.map_shared_rank(part, k) : part) + (w * ROWS + m) * L::LDO + d);
+                if (k < CS) x[k] = *reinterpret_cast<const float4*>((CS > 1 ? cluster.map_shared_rank(part, k) : part) + m * L::LDO + d);
             float mx = s_all[0][m].x, sum = 0.f;
             for (int k = 1; k < CS; ++k) mx = fmaxf(mx, s_all[k][m].x);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -913,24 +926,11 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
                     sum += f * ml.y;
                     acc.x += f * x[k].x; acc.y += f * x[k].y; acc.z += f * x[k].z; acc.w += f * x[k].w;
                 }
-            if constexpr (KW > 1) {
-                s_x[warp][lane] = acc;
-                __syncthreads();
-                if (w == 0)
-#pragma unroll
-                    for (int k = 1; k < KW; ++k) {
-                        const float4 y = s_x[warp + k][lane];
-                        acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
-                    }
-            }
-            if (w == 0 && i < valid) {
-                const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-                const float inv = inverse(sum);
-                *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
-                    make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
-                if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
-            }
-            if constexpr (KW > 1) __syncthreads();
+            const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
+            const float inv = inverse(sum);
+            *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
+                make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
+            if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
         }
         // (no block leaves while another reads its shared memory)
         if (CS > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -1160,14 +1160,16 @@ constexpr int W_KEYS = 512;          // slots of a block that adds weights
 
 // Blocks [0, n_join): a warp per query row adds the pieces of its output.  Blocks beyond: the weights of W_KEYS slots of a KV head,
 // exp(score - lse) summed over the rows and the heads of the group and added to what is there.
-template <typename T, int HD, int UNIT, bool WEIGHTS>
+template <typename T, int HD, int UNIT, bool SPLIT, bool WEIGHTS>
 __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_join, int groups) {
     constexpr int PER = HD / 32;     // columns of a lane
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, HR = a.kv.Hkv * a.RB;
     __shared__ float s_lse[MAX_ROWS_BLOCK];
+    __shared__ float s_acc[SPLIT ? 4 : 1][SPLIT ? HD : 1];
     pdl_wait();
     if ((int)blockIdx.x < n_join) {
-        const int seg = blockIdx.x / groups, m = (blockIdx.x - seg * groups) * 4 + warp, b = seg / HR, hr = seg - b * HR;
+        // a warp has a row, or (SPLIT) the block has one and its warps a quarter of the pieces each
+        const int seg = blockIdx.x / groups, m = SPLIT ? blockIdx.x - seg * groups : (blockIdx.x - seg * groups) * 4 + warp, b = seg / HR, hr = seg - b * HR;
         const Seq q = seq_of<UNIT>(a, b);
         const int h = hr / a.RB, row = (hr - h * a.RB) * a.rows_block + m;
         if (q.nt == 0 || m >= a.rows_block || row >= q.nb * a.G) return;
@@ -1177,8 +1179,9 @@ __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_joi
         float acc[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < p.n; ++i) {
+        const int each = SPLIT ? (p.n + 3) / 4 : p.n, p0 = SPLIT ? warp * each : 0, p1 = min(p0 + each, p.n);
+#pragma unroll 8
+        for (int i = p0; i < p1; ++i) {
             const long long at = place_of(p, i) * a.rows_block + m;
             const float mi = a.part_ml[at].x, f = mi == ml.x ? 1.f : ex2(mi - ml.x);
             const float* src = a.part_o + at * HD + lane * PER;
@@ -1188,6 +1191,16 @@ __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_joi
                 acc[k] += f * x.x;
                 acc[k + 1] += f * x.y;
             }
+        }
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) s_acc[warp][lane * PER + k] = acc[k];
+            __syncthreads();
+            if (warp > 0) return;
+#pragma unroll
+            for (int w = 1; w < 4; ++w)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) acc[k] += s_acc[w][lane * PER + k];
         }
         const int r = row / a.G, hq = h * a.G + row - r * a.G;
         const float inv = inverse(ml.y);
@@ -1312,7 +1325,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     }
     const long long heads = (long long)a.B * a.kv.Hkv * a.RB;
     if (heads * std::max(4 * tiles, (long long)MAX_CLUSTER) > 0x7fffffffll ||
-        heads * ((a.max_len + W_KEYS - 1) / W_KEYS) + heads * 16 > 0x7fffffffll) return MTAD_E_CAPACITY;
+        heads * ((a.max_len + W_KEYS - 1) / W_KEYS) + heads * MAX_ROWS_BLOCK > 0x7fffffffll) return MTAD_E_CAPACITY;
     // (workspace sizes may be asked for without a device)
     int sms = 148, dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) sms = 148;
@@ -1320,7 +1333,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     // A cluster per head where that takes few tiles a block
     int cs = 1;
     while (cs < MAX_CLUSTER && cs < tiles && heads * cs * 2 <= fill) cs *= 2;
-    const bool list = (tiles + cs - 1) / cs > CLUSTER_TILES || (a.weights && a.RB > 1);
+    const bool list = (tiles + cs - 1) / cs > (a.rows_block <= 16 ? CLUSTER_TILES : CLUSTER_TILES_WIDE) || (a.weights && a.RB > 1);
     a.cluster = list ? 0 : cs;
     a.even = kv->page_size % 16 == 0;
     a.dense = kv->slot_stride == kv->head_dim ? kv->head_dim : 0;
@@ -1380,12 +1393,18 @@ cudaError_t launch_hd(const AttnPlan& p, cudaStream_t st) {
     const cudaError_t e = launch_rows<T, HD, true>(p, st);
     if (e != cudaSuccess) return e;
     mtad_ops_count(1);
-    const int groups = (std::min(p.a.R * p.a.G, p.a.rows_block) + 3) / 4;
-    const int join = p.a.B * p.a.kv.Hkv * p.a.RB * groups;
+    // (a head in many pieces: 296 of them took one warp 45 us)
+    const long long heads = (long long)p.a.B * p.a.kv.Hkv * p.a.RB;
+    const bool split = p.a.grid / heads >= 12;
+    const int rows = std::min(p.a.R * p.a.G, p.a.rows_block), groups = split ? rows : (rows + 3) / 4, join = (int)heads * groups;
     const int add = p.a.weights ? p.a.B * p.a.kv.Hkv * ((p.a.max_len + W_KEYS - 1) / W_KEYS) : 0;
     auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(join + add), dim3(NT), 0, st, true, p.a, join, groups); };
-    return p.narrow ? (add ? go(join_kernel<T, HD, RW, true>) : go(join_kernel<T, HD, RW, false>))
-                    : (add ? go(join_kernel<T, HD, TK, true>) : go(join_kernel<T, HD, TK, false>));
+    auto pick = [&](auto unit) {
+        constexpr int U = decltype(unit)::value;
+        return split ? (add ? go(join_kernel<T, HD, U, true, true>) : go(join_kernel<T, HD, U, true, false>))
+                     : (add ? go(join_kernel<T, HD, U, false, true>) : go(join_kernel<T, HD, U, false, false>));
+    };
+    return p.narrow ? pick(std::integral_constant<int, RW>()) : pick(std::integral_constant<int, TK>());
 }
 template <typename T>
 cudaError_t launch_t(const AttnPlan& p, cudaStream_t st) {
