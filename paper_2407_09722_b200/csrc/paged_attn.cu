@@ -5,16 +5,21 @@
 //
 // What bounds it: a call reads the visible keys and values once (2 * 2 * head_dim bytes per token and KV head) and does 4 *
 // head_dim operations per query row with them, a few dozen per byte at most, so HBM bounds it and the tensor cores idle; at
-// short lengths launches and latency do.  Hence
-//  - the query rows of a KV head (rows x heads of the group) share one pass over its keys: they are the M side of the
-//    mma.sync tiles (m16n8k16), 16, 32 or 64 a block; the rest of the 16 costs tensor work that nobody waits for;
-//  - the work is a list of 64-key tiles over (sequence, KV head, row block) that is cut evenly over a grid that fills the
-//    GPU once, whatever the lengths: the batch may be ragged, a single long sequence may be alone.  A block's share
-//    may begin and end inside a head: its pieces (running maximum, sum, unnormalised output, all fp32) are joined by a
-//    second kernel that the first one's launch overlaps; heads that one block saw whole are finished there and then;
-//  - a warp copies the keys and values that it multiplies itself (16 rows per request of the tile, cp.async, three or more
-//    stages) where a block has 16 query rows, so that no barrier stands between a copy and its use;
-//  - page ids and offsets are looked up one tile ahead, a lane per key, and handed around by shuffles.
+// short lengths launches and latency do.  Hence mma.sync tiles (m16n8k16) straight from shared memory to registers, not tcgen05:
+// tensor memory would add two trips per tile and nothing waits for the products.
+//  - The query rows of a KV head (rows x heads of the group) share one pass over its keys.  Up to 16 of them (Narrow) keys stand on the
+//    M side; 17 to 64 (Wide) the queries do; more are cut into blocks of 64 rows, each with a pass of its own.
+//  - Long or ragged batches (stream_kernel for up to 16 rows, attn_kernel with LIST beyond): the list of tiles over (sequence, KV head, row
+//    block) is cut evenly over a grid that fills the GPU once.  Shares may begin and end inside a head: its pieces (reference, sum,
+//    unnormalised output, all fp32) are joined by a second kernel whose launch the first one overlaps.
+//  - Short contexts (attn_kernel without LIST): a cluster of up to eight blocks has a head and joins its pieces through distributed shared
+//    memory, one launch and no workspace.
+//  - Copies are cp.async, three or four stages, page ids looked up a tile ahead; with up to 16 query rows a warp multiplies what it has
+//    copied itself and no barrier stands in between.
+// Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 98 us, 5.5 TB/s (a plain read of 8 GB
+// runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 65 us, 5.2 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
+// one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
+// taken over from blocks not yet launched evened that out, and cost more than it gave), the second kernel (5 us), the first loads (4 us).
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as two terms of the cache's type
 // (p and what its rounding left), so the 2^-9 of a bf16 probability does not reach the output; the output is rounded once.
 #include <cooperative_groups.h>
@@ -36,7 +41,7 @@ constexpr int TK = 64;               // keys of a tile
 constexpr int NT = 128;              // threads of a block
 constexpr int MAX_ROWS_BLOCK = 64;   // query rows (rows x heads of the group) of a block
 constexpr int MAX_CLUSTER = 8;
-constexpr int CLUSTER_TILES = 12, CLUSTER_TILES_WIDE = 5;       // tiles of a block up to which a cluster has a head
+constexpr int CLUSTER_TILES = 12, CLUSTER_TILES_WIDE = 8;       // tiles of a block up to which a cluster has a head
 
 struct AttnArgs {
     PagedView kv;
@@ -149,7 +154,7 @@ template <int HD> __device__ __forceinline__ uint32_t at(int r, int c) { return 
 template <int HD, int ROWS> struct Tile {
     static constexpr int CH = HD / 8;                    // 16-byte pieces of a row
     static constexpr int BYTES = TK * HD * 2;            // keys (or values) of a tile
-    // two blocks on an SM (one with heads of 256): 70 to 105 KB of a block's shared memory on their way or in use
+    // two blocks on an SM (one with heads of 256): 64 to 96 KB of a block's shared memory (128 to 192) on their way or in use
     static constexpr int STAGES = HD == 64 ? 4 : ROWS <= 16 ? 3 : 2;
     static constexpr int BLOCKS = HD == 256 ? 1 : 2;
     static constexpr int MT = ROWS <= 16 ? 1 : ROWS / 16;                // warps over the rows; 4 / MT over the keys of a tile
@@ -397,17 +402,14 @@ template <typename T, int HD, int ROWS> struct Narrow {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
     }
-    // Puts (or adds) the columns [cb * HD / COLS, ..) of this warp's output to buf[row][ld]
-    __device__ __forceinline__ void put(float* buf, int ld, int, bool add) {
+    // Puts this warp's output to buf[row][ld]
+    __device__ __forceinline__ void put(float* buf, int ld, int, bool) {
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
             for (int n = 0; n < N8; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float* at = buf + (n * 8 + t2 + (e & 1)) * ld + d * 16 + (e >> 1) * 8 + g;
-                    *at = add ? *at + o[d][n][e] : o[d][n][e];
-                }
+                for (int e = 0; e < 4; ++e) buf[(n * 8 + t2 + (e & 1)) * ld + d * 16 + (e >> 1) * 8 + g] = o[d][n][e];
     }
 };
 
@@ -586,6 +588,7 @@ template <typename T, int HD, int ROWS> struct Wide {
             if (wk == 0 && (lane & 3) == 0) s_ml[row] = make_float2(to, sum);
         }
     }
+    // Puts (or adds) this warp's output to buf[row][ld]: all columns, or the part cb of them
     __device__ __forceinline__ void put(float* buf, int ld, int cb, bool add) {
         constexpr int NB = HD / 8 / L::COLS;
         const bool all = ld == L::LDO;                    // every column
@@ -963,8 +966,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
 }
 
 // Up to 16 query rows, the list cut over all warps of the GPU: a warp has an even share of the list of 16-key tiles and a ring of its own,
-// waits for nobody, and leaves its pieces of cut heads as they lie in its registers.  (With a block's four warps on one tile, their
-// outputs were added at the end of every share and head: 1.3 us each time in which the block's copies ran dry.)
+// waits for nobody, and writes its pieces of cut heads from its registers.
 template <int HD, int ROWS> struct Ring {
     static constexpr int BYTES = RW * HD * 2, STAGES = Tile<HD, ROWS>::STAGES;
     static constexpr int SMEM = (NT / 32) * STAGES * 2 * BYTES;

@@ -583,9 +583,9 @@ int mtad_paged_evict(const mtad_paged_kv* kv, const mtad_paged_eviction* c, void
         mtad_ops_count(1);
     }
     if (e == cudaSuccess && a.max_len > a.keep) {
-        // two tensors; parts of a row only where SMs would go without a block
+        // two tensors; parts of a row, of 64 bytes at least, only where SMs would go without a block
         int slices = 2;
-        while (slices < 16 && heads * slices < sms) slices *= 2;
+        while (slices < 16 && heads * slices < sms && kv->head_dim * 2 / slices >= 64) slices *= 2;
         // (a part of a row has at least one piece of 16 bytes where it has any)
         const int least = std::max(kv->head_dim / 8 * 2 / slices, 1);
         e = ops_smem<move_kernel>(MV_SMEM);
