@@ -9,9 +9,9 @@
 //
 // Every row is read once for its log-sum-exp, one row and the uniforms again for the draw: bound by those bytes together with the
 // exponentials (16 a clock and SM: 24 us of 64 sequences x 13 rows x 128000 bf16 logits whose bytes take 33), at small
-// batches by latency.  A cluster of eight blocks has a sequence, a block an eighth of the vocabulary; warps take (row, part) tasks, a
+// batches by latency.  A cluster of four or eight blocks has a sequence, a block its part of the vocabulary; warps take (row, part) tasks, a
 // reference and a sum a lane; rows' statistics and the draw's candidates cross the cluster in distributed shared memory, so
-// the call is one launch and needs no workspace.  Statistics are fp32, merged in a fixed order.  The batch of 64 takes 64 us (3.8 TB/s;
+// the call is one launch and needs no workspace.  Statistics are fp32, merged in a fixed order.  The batch of 64 takes 60 us (4.1 TB/s;
 // 14 of them the draw, whose loads wait for the accepted prefix), one chain of 5 rows of 32000 fp32 logits 11 us.
 #include <cooperative_groups.h>
 #include <math.h>
@@ -25,7 +25,6 @@ namespace mtad {
 
 namespace {
 
-constexpr int AC_CLUSTER = 8;
 constexpr int AC_ROWS = 2 * MTAD_MAX_DEPTH + 1, AC_PARTS = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -209,13 +208,14 @@ __device__ __forceinline__ void better(Best& a, float y, int v) {
     if (y > a.y || (y == a.y && v < a.v)) { a.y = y; a.v = v; }
 }
 
-// THREADS: 512 where clusters are few and latency counts, 256 where they fill the GPU (more of them at work at once)
-template <typename T, int THREADS>
-__global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 / THREADS) accept_rows_kernel(const AcceptRowsArgs a) {
+// CLUSTER blocks of THREADS threads a sequence: eight of 512 where that leaves SMs idle, four of 512 up to two blocks an SM (64 sequences:
+// 60.5 us; eight of 256: 64), four of 256 beyond
+template <typename T, int CLUSTER, int THREADS>
+__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 / THREADS) accept_rows_kernel(const AcceptRowsArgs a) {
     constexpr int WARPS = THREADS / 32;
-    constexpr bool few = THREADS == 512;
+    constexpr bool few = CLUSTER == 8;
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), b = blockIdx.x / AC_CLUSTER, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster.block_rank(), b = blockIdx.x / CLUSTER, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ Stat s_part[AC_ROWS * AC_PARTS];
     __shared__ Stat s_row[AC_ROWS];                       // read by the cluster
     __shared__ Best s_best[WARPS], s_block;            // s_block: read by the cluster
@@ -229,7 +229,7 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 10
     const int rows = g + 1 + (spd ? g : 0);
     const T* z = static_cast<const T*>(a.z) + (long long)b * a.z_sb;
     const T* q = spd ? static_cast<const T*>(a.q) + (long long)b * a.q_sb : nullptr;
-    const int per = ((V + AC_CLUSTER - 1) / AC_CLUSTER + 7) / 8 * 8, v0 = min(rank * per, V), v1 = min(v0 + per, V);
+    const int per = ((V + CLUSTER - 1) / CLUSTER + 7) / 8 * 8, v0 = min(rank * per, V), v1 = min(v0 + per, V);
     // tokens and their logits, early: a lane per drafted token
     uint32_t bits = given == g ? 0u : MTAD_ST_BAD_COUNT;
     int x = 0;
@@ -277,7 +277,7 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 10
     cluster.sync();
     if (tid < rows) {
         Stat st = *cluster.map_shared_rank(&s_row[tid], 0);
-        for (int k = 1; k < AC_CLUSTER; ++k) st = merge(st, *cluster.map_shared_rank(&s_row[tid], k));
+        for (int k = 1; k < CLUSTER; ++k) st = merge(st, *cluster.map_shared_rank(&s_row[tid], k));
         s_lse[tid] = (st.m + log2f(st.s)) * LN2;
     }
     __syncthreads();
@@ -410,7 +410,7 @@ __global__ void __cluster_dims__(AC_CLUSTER, 1, 1) __launch_bounds__(THREADS, 10
         cluster.sync();
         best = Best{-CUDART_INF_F, 0x7fffffff};
 #pragma unroll
-        for (int k = 0; k < AC_CLUSTER; ++k) {
+        for (int k = 0; k < CLUSTER; ++k) {
             const Best c = *cluster.map_shared_rank(&s_block, k);
             better(best, c.y, c.v);
         }
@@ -450,13 +450,16 @@ int accept_rows(const mtad_accept_rows* c, const float* draft_logq, float log_ta
     a.gamma = c->gamma; a.V = c->vocab;
     a.out = *out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const dim3 grid(c->batch * AC_CLUSTER);
     mtad_ops_count(1);
-    const bool few = c->batch * AC_CLUSTER <= 296;
-    auto launch = [&](auto wide, auto slim) { return few ? launch_pdl(wide, grid, dim3(512), 0, st, true, a) : launch_pdl(slim, grid, dim3(256), 0, st, true, a); };
-    return ops_status(c->dtype == MTAD_F32    ? launch(accept_rows_kernel<float, 512>, accept_rows_kernel<float, 256>)
-                      : c->dtype == MTAD_BF16 ? launch(accept_rows_kernel<__nv_bfloat16, 512>, accept_rows_kernel<__nv_bfloat16, 256>)
-                                              : launch(accept_rows_kernel<__half, 512>, accept_rows_kernel<__half, 256>));
+    int sms = 148, dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) sms = 148;
+    auto launch = [&](auto type) {
+        using T = decltype(type);
+        if (c->batch * 8 <= sms) return launch_pdl(accept_rows_kernel<T, 8, 512>, dim3(c->batch * 8), dim3(512), 0, st, true, a);
+        if (c->batch * 4 <= 2 * sms) return launch_pdl(accept_rows_kernel<T, 4, 512>, dim3(c->batch * 4), dim3(512), 0, st, true, a);
+        return launch_pdl(accept_rows_kernel<T, 4, 256>, dim3(c->batch * 4), dim3(256), 0, st, true, a);
+    };
+    return ops_status(c->dtype == MTAD_F32 ? launch(0.f) : c->dtype == MTAD_BF16 ? launch(__nv_bfloat16()) : launch(__half()));
 }
 
 }  // namespace

@@ -559,7 +559,8 @@ def rows_of(seed, B, D, V, dtype):
 
 @pytest.mark.parametrize("rule", ["mtad", "spd"])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
-@pytest.mark.parametrize("B,D,V", [(1, 1, 1), (3, 1, 7), (1, 4, 64), (5, 3, 1009), (2, 32, 515), (9, 6, 32000), (2, 2, 100003)])
+@pytest.mark.parametrize("B,D,V", [(1, 1, 1), (3, 1, 7), (1, 4, 64), (5, 3, 1009), (2, 32, 515), (9, 6, 32000), (30, 2, 777), (100, 1, 300),
+                                   (2, 2, 100003)])
 def test_accept_rows(rule, dtype, B, D, V):
     """Vocabularies of one token, smaller than a cluster, odd (rows begin off 16 bytes), large; one to 32 drafted tokens."""
     z, dr, tok, u, ua, logq = rows_of(B * V + D, B, D, V, DT[dtype])
