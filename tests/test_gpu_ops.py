@@ -827,3 +827,36 @@ def test_calls_from_two_threads_on_two_streams():
     for k in range(2):
         for a, b in zip(alone[k], both[k]):
             assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("batch,hq,hkv,rows,page,window,hd", [(300, 1, 1, 1, 16, 0, 64), (300, 2, 1, 5, 5, 0, 64), (70, 32, 8, 1, 16, 1000, 64),
+                                                              (300, 20, 1, 1, 16, 0, 64), (100, 12, 2, 4, 24, 900, 128), (40, 8, 8, 2, 64, 0, 256)])
+def test_attention_many_sequences_over_a_cut_list(batch, hq, hkv, rows, page, window, hd):
+    """More sequences than a warp has lanes, some empty, some long: the list of tiles is found by more than one sequence a lane, with a window
+    too, for few and many query rows a head, on even and uneven pages."""
+    g = torch.Generator().manual_seed(batch + hq)
+    lens = [int(n) for n in torch.randint(0, 2000, (batch,), generator=g)]
+    lens[0], lens[1], lens[-1] = 0, 1999, 0
+    lens[5:9] = [0, 1, 16, 17]
+    c = Cache(70, lens, hkv, hd, page)
+    check_attention(c, queries(70, batch, rows, hq, hd, torch.bfloat16), window=window, sinks=3 if window else 0)
+
+
+def test_attention_as_many_rows_as_a_call_takes():
+    """256 rows of a prompt chunk on grouped heads: 32 blocks of query rows a KV head."""
+    c = Cache(71, [300, 256, 100], 1, 64, 16)
+    check_attention(c, queries(71, 3, 256, 8, 64, torch.bfloat16), n_rows=[256, 256, 77])
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_by_a_cluster_a_head(in_place):
+    c = Cache(72, [40000, 39000], 1, 8, 64)
+    s = torch.rand(2, 1, 40000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)).mul(50).round()      # many equal scores
+    check_evict(c, s, 12345, 5, 1000, in_place)
+
+
+def test_launches_are_counted():
+    c = Cache(73, [20], 1, 64, 16)
+    n = M.mtad_kernel_launches()
+    M.paged_attention(queries(73, 1, 1, 1, 64, torch.bfloat16), *c.args(), c.lens)
+    assert M.mtad_kernel_launches() == n + 1
