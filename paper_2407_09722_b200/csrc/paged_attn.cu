@@ -668,7 +668,7 @@ template <typename T, int HD, int ROWS, bool LIST>
 __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const AttnArgs a) {
     using L = Tile<HD, ROWS>;
     using Core = typename std::conditional<(ROWS <= 16), Narrow<T, HD, ROWS>, Wide<T, HD, ROWS>>::type;
-    constexpr int KW = Core::KW, S = L::STAGES, CH = L::CH, PASS = 32 / CH;
+    constexpr int KW = Core::KW, S = L::STAGES, CH = L::CH;
     constexpr bool OWN = ROWS <= 16;                      // a warp multiplies the rows that it has copied itself
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ float2 s_part[KW * ROWS];
@@ -975,7 +975,7 @@ template <typename T, int HD, int ROWS>
 __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(const AttnArgs a) {
     using L = Ring<HD, ROWS>;
     using Core = Narrow<T, HD, ROWS>;
-    constexpr int S = L::STAGES, CH = HD / 8, PASS = 32 / CH;
+    constexpr int S = L::STAGES, CH = HD / 8;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.x * (NT / 32) + warp;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * S * 2 * L::BYTES;
