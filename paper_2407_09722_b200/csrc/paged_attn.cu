@@ -16,8 +16,8 @@
 //    memory, one launch and no workspace.
 //  - Copies are cp.async, three or four stages, page ids looked up a tile ahead; with up to 16 query rows a warp multiplies what it has
 //    copied itself and no barrier stands in between.
-// Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 98 us, 5.5 TB/s (a plain read of 8 GB
-// runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 65 us, 5.2 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
+// Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 93 us, 5.8 TB/s (a plain read of 8 GB
+// runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 61 us, 5.6 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
 // one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
 // taken over from blocks not yet launched evened that out, and cost more than it gave), the second kernel (5 us), the first loads (4 us).
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as two terms of the cache's type
@@ -111,8 +111,16 @@ __device__ __forceinline__ void advance(const AttnArgs& a, Cursor& c) {
     } while (c.s.nt == 0);
 }
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
+}
+// What is read once leaves the L2 first (a long list: 61 us instead of 65 for the ragged batch of eight); what a short call has read may be there
+// when the next one asks for it, and rows in several blocks read it again.
+__device__ __forceinline__ uint64_t copy_policy(bool once) {
+    uint64_t p;
+    if (once) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    return p;
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -621,7 +629,7 @@ __device__ __forceinline__ Spot look_up(const AttnArgs& a, const Seq& s, int b, 
 // A warp brings 16 rows of keys and values (`apart` bytes further on) of a KV head that begins at `head` of a page.
 template <int HD>
 __device__ __forceinline__ void copy_rows(const AttnArgs& a, const Spot& at_, int b, long long head, uint32_t tile, int apart, int c_row, int c_col,
-                                          int chunks) {
+                                          int chunks, uint64_t policy) {
     constexpr int CH = HD / 8, PASS = 32 / CH;
     const uint32_t to = tile + c_row * HD * 2, piece = (c_col ^ c_row) << 4;      // (c_row < PASS <= 4: at() of row p * PASS + c_row)
     auto dst = [&](int p) { return to + p * PASS * HD * 2 + (piece ^ (((p * PASS) & 7) << 4)); };
@@ -633,8 +641,8 @@ __device__ __forceinline__ void copy_rows(const AttnArgs& a, const Spot& at_, in
             const uint16_t *k = a.kv.k + e, *v = a.kv.v + e;
 #pragma unroll
             for (int p = 0; p < 16 / PASS; ++p) {
-                cp16(dst(p), k + p * PASS * HD, true);
-                cp16(dst(p) + apart, v + p * PASS * HD, true);
+                cp16(dst(p), k + p * PASS * HD, true, policy);
+                cp16(dst(p) + apart, v + p * PASS * HD, true, policy);
             }
         } else {
             const bool in = c_col < chunks;
@@ -642,8 +650,8 @@ __device__ __forceinline__ void copy_rows(const AttnArgs& a, const Spot& at_, in
             const long long step = in ? PASS * a.kv.slot_stride : 0;
 #pragma unroll
             for (int p = 0; p < 16 / PASS; ++p, k += step, v += step) {
-                cp16(dst(p), k, in);
-                cp16(dst(p) + apart, v, in);
+                cp16(dst(p), k, in, policy);
+                cp16(dst(p) + apart, v, in, policy);
             }
         }
     } else {
@@ -653,8 +661,8 @@ __device__ __forceinline__ void copy_rows(const AttnArgs& a, const Spot& at_, in
         for (int p = 0; p < 16 / PASS; ++p) {
             const long long o = __shfl_sync(0xffffffffu, off, p * PASS + c_row);
             const bool in = o >= 0 && c_col < chunks;
-            cp16(dst(p), a.kv.k + (in ? o + c_col * 8 : 0), in);
-            cp16(dst(p) + apart, a.kv.v + (in ? o + c_col * 8 : 0), in);
+            cp16(dst(p), a.kv.k + (in ? o + c_col * 8 : 0), in, policy);
+            cp16(dst(p) + apart, a.kv.v + (in ? o + c_col * 8 : 0), in, policy);
         }
     }
 }
@@ -777,9 +785,10 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
 
     // ---- copies: a warp brings rows 16 * warp .. + 15 of a tile
     const int c_row = lane / CH, c_col = lane % CH;       // this lane's row and piece in a request
+    const uint64_t policy = copy_policy(false);
     auto find = [&](const Cursor& c) { return look_up(a, c.s, c.b, (c.t < c.s.ns ? c.t : c.t + c.s.skip) * TK + warp * RW + (lane & 15)); };
     auto copy = [&](const Spot& spot, const Cursor& c, int stage) {
-        copy_rows<HD>(a, spot, c.b, (long long)(c.hr / a.RB) * a.kv.head_stride, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks);
+        copy_rows<HD>(a, spot, c.b, (long long)(c.hr / a.RB) * a.kv.head_stride, sm + stage * 2 * L::BYTES + warp * RW * HD * 2, L::BYTES, c_row, c_col, chunks, policy);
     };
     int ahead = 0;                                        // tiles handed to the copies
     Spot spot{-1, 0}, begin[S - 1];
@@ -1037,9 +1046,10 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
         }
     };
     const int c_row = lane / CH, c_col = lane % CH;
+    const uint64_t policy = copy_policy(true);
     auto find = [&](const Cursor& c) { return look_up(a, c.s, c.b, (c.t < c.s.ns ? c.t : c.t + c.s.skip) * RW + (lane & 15)); };
     auto copy = [&](const Spot& spot, const Cursor& c, int stage) {
-        copy_rows<HD>(a, spot, c.b, c.hr * a.kv.head_stride, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks);
+        copy_rows<HD>(a, spot, c.b, c.hr * a.kv.head_stride, ring + stage * 2 * L::BYTES, L::BYTES, c_row, c_col, chunks, policy);
     };
     int ahead = 0;
     Spot spot{-1, 0}, begin[S - 1];
