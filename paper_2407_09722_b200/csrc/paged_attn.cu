@@ -1187,21 +1187,50 @@ __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_joi
         if (q.nt == 0 || m >= a.rows_block || row >= q.nb * a.G) return;
         const Pieces p = pieces_of(a, q, b, hr);
         if (p.n == 1) return;
-        const float2 ml = joined(a, p, m, lane);
+        float2 ml;
         float acc[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-        const int each = SPLIT ? (p.n + 3) / 4 : p.n, p0 = SPLIT ? warp * each : 0, p1 = min(p0 + each, p.n);
-#pragma unroll 8
-        for (int i = p0; i < p1; ++i) {
-            const long long at = place_of(p, i) * a.rows_block + m;
-            const float mi = a.part_ml[at].x, f = mi == ml.x ? 1.f : ex2(mi - ml.x);
-            const float* src = a.part_o + at * HD + lane * PER;
+        if (!SPLIT && p.n <= 8) {                         // outputs and statistics are asked for together
+            const float2 mine = lane < p.n ? a.part_ml[place_of(p, lane) * a.rows_block + m] : make_float2(-CUDART_INF_F, 0.f);
+            float x[8][PER];
 #pragma unroll
-            for (int k = 0; k < PER; k += 2) {
-                const float2 x = *reinterpret_cast<const float2*>(src + k);
-                acc[k] += f * x.x;
-                acc[k + 1] += f * x.y;
+            for (int i = 0; i < 8; ++i) {
+                const float* src = a.part_o + (place_of(p, min(i, p.n - 1)) * a.rows_block + m) * HD + lane * PER;
+                if (i < p.n)
+#pragma unroll
+                    for (int k = 0; k < PER; k += 2) *reinterpret_cast<float2*>(&x[i][k]) = *reinterpret_cast<const float2*>(src + k);
+            }
+            ml.x = mine.x;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) ml.x = fmaxf(ml.x, __shfl_xor_sync(0xffffffffu, ml.x, o));
+            ml.x = __shfl_sync(0xffffffffu, ml.x, 0);
+            const float f = mine.x == ml.x ? 1.f : ex2(mine.x - ml.x);
+            ml.y = lane < p.n ? mine.y * f : 0.f;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) ml.y += __shfl_xor_sync(0xffffffffu, ml.y, o);
+            ml.y = __shfl_sync(0xffffffffu, ml.y, 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float fi = __shfl_sync(0xffffffffu, f, i);
+                if (i < p.n)
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) acc[k] += fi * x[i][k];
+            }
+        } else {
+            ml = joined(a, p, m, lane);
+            const int each = SPLIT ? (p.n + 3) / 4 : p.n, p0 = SPLIT ? warp * each : 0, p1 = min(p0 + each, p.n);
+#pragma unroll 8
+            for (int i = p0; i < p1; ++i) {
+                const long long at = place_of(p, i) * a.rows_block + m;
+                const float mi = a.part_ml[at].x, f = mi == ml.x ? 1.f : ex2(mi - ml.x);
+                const float* src = a.part_o + at * HD + lane * PER;
+#pragma unroll
+                for (int k = 0; k < PER; k += 2) {
+                    const float2 x = *reinterpret_cast<const float2*>(src + k);
+                    acc[k] += f * x.x;
+                    acc[k + 1] += f * x.y;
+                }
             }
         }
         if constexpr (SPLIT) {
