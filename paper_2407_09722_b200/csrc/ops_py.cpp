@@ -93,6 +93,7 @@ struct Pages {
                           "k_pages and v_pages: [pages, kv heads, slots of a page, head_dim], alike in shape, strides, type and device");
         TORCH_CHECK_VALUE(t.dim() == 2 && t.scalar_type() == at::kInt && t.device() == k.device() && t.stride(1) == 1 && t.size(0) >= batch,
                           "table: int32 [sequences, pages] on the pages' device, a row for every sequence, a row contiguous");
+        TORCH_CHECK_VALUE(t.size(0) <= 1 || t.stride(0) >= t.size(1), "table: rows lie apart, each of its own (of an expanded view: table.contiguous())");
         TORCH_CHECK_VALUE(k.stride(3) == 1 && (type_of(k) == MTAD_BF16 || type_of(k) == MTAD_F16), "pages hold rows of bf16 or fp16 that are contiguous");
         kv.k_pages = k.data_ptr();
         kv.v_pages = v.data_ptr();
@@ -100,7 +101,7 @@ struct Pages {
         kv.page_stride = step(k, 0);
         kv.head_stride = step(k, 1);
         kv.slot_stride = k.size(2) == 1 ? k.size(3) : k.stride(2);
-        kv.table_stride = std::max(t.stride(0), t.size(1));               // (of one row: whatever)
+        kv.table_stride = t.size(0) <= 1 ? t.size(1) : t.stride(0);       // (of one row: whatever)
         kv.dtype = type_of(k);
         kv.n_pages = (int32_t)std::min<int64_t>(k.size(0), INT32_MAX);
         kv.page_size = (int32_t)std::min<int64_t>(k.size(2), INT32_MAX);
