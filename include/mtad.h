@@ -330,7 +330,8 @@ int mtad_debug_set_path(mtad_ctx* ctx, int path);
  * page table[b * table_stride + j / page_size].  Element d of (page, head, slot) lies at page * page_stride + head *
  * head_stride + slot * slot_stride + d of k_pages, and in the same place of v_pages.  All strides count elements and are
  * multiples of 8, both pointers 16-byte aligned.  One layer of the contiguous cache above is such a cache: page_size =
- * kv_capacity, table[b] = b.  Sequences may share pages that are only read. */
+ * kv_capacity, table[b] = b.  Sequences may share pages that are only read.  Arrays that a call writes (the pages of an append or an
+ * eviction, which keys and values do not share either) hold no element in two places: strides at least as long as what they stride over, else MTAD_E_INVALID. */
 enum { MTAD_BF16 = 0, MTAD_F16 = 1, MTAD_F32 = 2 };
 #define MTAD_PAGED_MAX_BATCH 4096       /* sequences per call */
 #define MTAD_PAGED_MAX_HEADS 1024

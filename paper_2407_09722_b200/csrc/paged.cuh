@@ -88,6 +88,35 @@ template <> struct Num<__half> {
     static constexpr uint32_t kExp = 0x7c00u;
 };
 
+// Host side: whether the elements of an array that a call writes all lie apart, rows of `inner` of them along the given dimensions (strides >= 0;
+// one that is not longer than what it strides over would have two threads write the same place).
+struct Dim {
+    int64_t count, stride;
+};
+template <int N>
+inline bool lie_apart(int64_t inner, Dim (&&d)[N]) {
+    for (int i = 1; i < N; ++i)                          // by stride
+        for (int k = i; k > 0 && d[k].stride < d[k - 1].stride; --k) {
+            const Dim x = d[k];
+            d[k] = d[k - 1];
+            d[k - 1] = x;
+        }
+    for (const Dim& x : d)
+        if (x.count < 1) return true;                     // (nothing there)
+    __int128 extent = inner;
+    for (const Dim& x : d) {
+        if (x.count == 1) continue;
+        if (x.stride < extent) return false;
+        extent += (__int128)x.stride * (x.count - 1);
+    }
+    return true;
+}
+// ... of the pages, for calls that write them
+inline bool pages_lie_apart(const mtad_paged_kv* kv) {
+    return kv->k_pages != kv->v_pages &&
+           lie_apart(kv->head_dim, {{kv->n_pages, kv->page_stride}, {kv->n_kv_heads, kv->head_stride}, {kv->page_size, kv->slot_stride}});
+}
+
 // Host side: checks of a mtad_paged_kv that every operator makes, and the kernels' view of it.
 inline int paged_view(const mtad_paged_kv* kv, PagedView* out) {
     if (!kv || !kv->k_pages || !kv->v_pages || !kv->table) return MTAD_E_INVALID;

@@ -1352,6 +1352,8 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     a.B = c->batch; a.R = c->rows; a.G = c->n_q_heads / kv->n_kv_heads;
     a.window = c->window; a.sinks = c->window > 0 ? c->sinks : 0;
     a.max_len = (int)std::min((long long)c->max_len, (long long)kv->max_pages * kv->page_size);
+    if (!lie_apart(kv->head_dim, {{a.B, a.o_sb}, {a.R, a.o_sr}, {c->n_q_heads, a.o_sh}})) return MTAD_E_INVALID;
+    if (c->weights && !lie_apart(a.max_len, {{a.B, c->weights_stride_seq}, {kv->n_kv_heads, c->weights_stride_head}})) return MTAD_E_INVALID;
     if (a.window >= a.max_len) a.window = a.sinks = 0;    // (every slot is inside it)
     a.scale2 = (float)((c->scale > 0.f ? (double)c->scale : 1.0 / sqrt((double)kv->head_dim)) * 1.4426950408889634);
     a.weights = c->weights; a.w_sb = c->weights_stride_seq; a.w_sh = c->weights_stride_head;

@@ -504,6 +504,7 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* c, void* s
         if (in[i] < 0 || in[i] % (c->dtype == MTAD_F32 ? 4 : 8)) return MTAD_E_INVALID;
     for (int i = 0; i < 3; ++i)
         if (outs[i] < 0 || outs[i] % 8) return MTAD_E_INVALID;
+    if (!pages_lie_apart(kv) || !lie_apart(kv->head_dim, {{c->batch, outs[0]}, {c->rows, outs[1]}, {c->n_q_heads, outs[2]}})) return MTAD_E_INVALID;
     a.lens = c->lens; a.n_rows = c->n_rows; a.pos = c->pos;
     a.q = c->q; a.k = c->k; a.v = c->v; a.q_out = static_cast<uint16_t*>(c->q_out);
     a.q_sb = in[0]; a.q_sr = in[1]; a.q_sh = in[2]; a.k_sb = in[3]; a.k_sr = in[4]; a.k_sh = in[5];
@@ -562,6 +563,8 @@ int mtad_paged_evict(const mtad_paged_kv* kv, const mtad_paged_eviction* c, void
     const int chunk = ((a.max_len + a.cluster - 1) / a.cluster + 3) & ~3;
     a.staged = chunk <= EV_STAGE;
     if (!a.staged && c->scores_out == c->scores) return MTAD_E_UNIMPLEMENTED;      // read again after places are written
+    if (!pages_lie_apart(kv) || (c->scores_out && !lie_apart(std::min(a.keep, a.max_len), {{c->batch, a.o_sb}, {kv->n_kv_heads, a.o_sh}})))
+        return MTAD_E_INVALID;
     const int smem = a.staged ? chunk * (int)sizeof(float) : 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = ops_smem<select_kernel>(EV_STAGE * (int)sizeof(float));

@@ -1,8 +1,11 @@
 """Layouts that the operators around a decoder of the caller's own cannot use, refused on the host."""
+import ctypes as C
+
 import pytest
 import torch
 
 import paper_2407_09722_b200 as M
+from paper_2407_09722_b200 import binding as Bn
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -39,3 +42,71 @@ def test_table_rows_that_lie_apart_are_taken(table):
     for call in _calls(k, table, torch.zeros(b, dtype=torch.int32), b):
         with pytest.raises(ValueError, match="CUDA tensors only"):
             call()
+
+
+# ---- arrays that a call writes: no element twice
+
+def _kv(**kw):
+    d = dict(k_pages=1 << 20, v_pages=2 << 20, table=256, page_stride=2 * 8 * 16 * 128, head_stride=16 * 128, slot_stride=128, table_stride=64,
+             dtype=0, n_pages=100, page_size=16, n_kv_heads=8, head_dim=128, max_pages=64)
+    d.update(kw)
+    return Bn.PagedKV(**d)
+
+
+def _attn(**kw):
+    d = dict(lens=256, q=4096, out=8192, q_stride_seq=3 * 8192, q_stride_row=8192, q_stride_head=128, out_stride_seq=3 * 8192, out_stride_row=8192,
+             out_stride_head=128, batch=2, rows=3, n_q_heads=64, max_len=1000)
+    d.update(kw)
+    return Bn.PagedAttn(**d)
+
+
+def _rows(**kw):
+    d = dict(lens=256, q=4096, k=8192, v=16384, q_out=4096, q_stride_seq=3 * 8192, q_stride_row=8192, q_stride_head=128, kv_stride_seq=3 * 1024,
+             kv_stride_row=1024, kv_stride_head=128, out_stride_seq=3 * 8192, out_stride_row=8192, out_stride_head=128, batch=2, rows=3, n_q_heads=64)
+    d.update(kw)
+    return Bn.PagedRows(**d)
+
+
+def _evict(**kw):
+    d = dict(lens=256, scores=4096, kept=8192, new_lens=512, scores_out=16384, scores_stride_seq=8000, scores_stride_head=1000, out_stride_seq=800,
+             out_stride_head=100, batch=2, max_len=1000, keep=100)
+    d.update(kw)
+    return Bn.PagedEviction(**d)
+
+
+W = dict(weights=1024, weights_stride_seq=8000, weights_stride_head=1000)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), 0), (W, 0), (dict(out_stride_seq=128, out_stride_head=256, out_stride_row=64 * 256), 0),          # [rows][heads][sequences]
+    (dict(rows=1, out_stride_row=0), 0), (dict(batch=1, out_stride_seq=0), 0), ({**W, "batch": 1, "weights_stride_seq": 0}, 0),
+    (dict(out_stride_seq=0), Bn.MTAD_E_INVALID), (dict(out_stride_row=0), Bn.MTAD_E_INVALID), (dict(out_stride_head=0), Bn.MTAD_E_INVALID),
+    (dict(out_stride_head=120), Bn.MTAD_E_INVALID), (dict(out_stride_seq=2 * 8192), Bn.MTAD_E_INVALID),
+    (dict(out_stride_seq=(1 << 62) + 8, out_stride_row=1 << 62, batch=3), Bn.MTAD_E_INVALID),
+    ({**W, "weights_stride_seq": 0}, Bn.MTAD_E_INVALID), ({**W, "weights_stride_head": 0}, Bn.MTAD_E_INVALID),
+    ({**W, "weights_stride_head": 999}, Bn.MTAD_E_INVALID), ({**W, "weights_stride_seq": 7999}, Bn.MTAD_E_INVALID)])
+def test_attention_outputs_that_overlap_themselves(lib, kw, code):
+    n = C.c_size_t(0)
+    assert lib.mtad_paged_attention_workspace(_kv(), _attn(**kw), C.byref(n)) == code
+
+
+PAGES = [dict(page_stride=0), dict(head_stride=0), dict(slot_stride=128, head_stride=128), dict(page_stride=16 * 128), dict(v_pages=1 << 20)]
+
+
+@pytest.mark.parametrize("kw", PAGES)
+def test_pages_that_overlap_are_read_but_not_written(lib, kw):
+    """Attention may read an expanded view of the pages; rows are not stored into one, nor moved in it."""
+    n = C.c_size_t(0)
+    assert lib.mtad_paged_attention_workspace(_kv(**kw), _attn(), C.byref(n)) == 0
+    assert lib.mtad_paged_append(_kv(**kw), _rows(), None) == Bn.MTAD_E_INVALID
+    assert lib.mtad_paged_evict(_kv(**kw), _evict(), None) == Bn.MTAD_E_INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(out_stride_seq=0), dict(out_stride_row=0), dict(out_stride_head=0), dict(out_stride_row=8184)])
+def test_append_queries_that_overlap_themselves(lib, kw):
+    assert lib.mtad_paged_append(_kv(), _rows(**kw), None) == Bn.MTAD_E_INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(out_stride_seq=0), dict(out_stride_head=0), dict(out_stride_head=99), dict(out_stride_seq=799)])
+def test_eviction_scores_that_overlap_themselves(lib, kw):
+    assert lib.mtad_paged_evict(_kv(), _evict(**kw), None) == Bn.MTAD_E_INVALID
