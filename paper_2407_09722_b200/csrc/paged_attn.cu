@@ -1363,7 +1363,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     a.RB = (M + a.rows_block - 1) / a.rows_block;
     long long tiles = (a.max_len + TK - 1) / TK;          // of 64 keys
     if (a.window > 0) {
-        const long long some = (long long)(a.sinks + TK - 1) / TK + ((long long)a.window + a.R + TK - 2) / TK + 1;
+        const long long some = ((long long)a.sinks + TK - 1) / TK + ((long long)a.window + a.R + TK - 2) / TK + 1;
         tiles = some < tiles ? some : tiles;
     }
     const long long heads = (long long)a.B * a.kv.Hkv * a.RB;

@@ -110,3 +110,12 @@ def test_append_queries_that_overlap_themselves(lib, kw):
 @pytest.mark.parametrize("kw", [dict(out_stride_seq=0), dict(out_stride_head=0), dict(out_stride_head=99), dict(out_stride_seq=799)])
 def test_eviction_scores_that_overlap_themselves(lib, kw):
     assert lib.mtad_paged_evict(_kv(), _evict(**kw), None) == Bn.MTAD_E_INVALID
+
+
+@pytest.mark.parametrize("sinks", [2 ** 31 - 1, 2 ** 31 - 63, 2 ** 31 - 64, 1024])
+def test_as_many_sinks_as_there_are_slots_or_more(lib, sinks):
+    """A window behind which every slot is a sink: the workspace of the whole cache."""
+    n, m = C.c_size_t(0), C.c_size_t(0)
+    call = dict(W, rows=40, out_stride_seq=40 * 8192, window=100, max_len=1000)
+    assert lib.mtad_paged_attention_workspace(_kv(), _attn(**{**call, "window": 0}), C.byref(n)) == 0
+    assert lib.mtad_paged_attention_workspace(_kv(), _attn(sinks=sinks, **call), C.byref(m)) == 0 and m.value == n.value
