@@ -20,8 +20,8 @@
 // runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 61 us, 5.6 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
 // one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
 // taken over from blocks not yet launched evened that out, and cost more than it gave), the second kernel (5 us), the first loads (4 us).
-// Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as two terms of the cache's type
-// (p and what its rounding left), so the 2^-9 of a bf16 probability does not reach the output; the output is rounded once.
+// Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as terms of the cache's type (p, and what
+// its rounding left; see Prob), so that they keep the bits of fp32; the output is rounded once.
 #include <cooperative_groups.h>
 #include <limits.h>
 #include <math_constants.h>
@@ -215,6 +215,14 @@ __device__ __forceinline__ void zero_mixed(const AttnArgs& a, const TileAt& t, i
 // and most tiles need neither a maximum over lanes nor a rescaling.
 constexpr float RAISE = 6.f;
 
+// Terms of the cache's type as which a probability enters the second product: three of bf16 hold the 24 bits of fp32, two of fp16 hold 22.
+// (Two of bf16 left 2^-18 of a probability out, which turned the rounding of one output in 2000.  The third takes no time where memory bounds
+// the call, up to 16 query rows a KV head; a chain of 5 on groups of 8, eight ragged sequences, takes 42.8 us instead of 37.9, four prompt
+// chunks of 256 rows at 2000 to 4000 slots 588 instead of 498.)
+template <typename T> struct Prob;
+template <> struct Prob<__nv_bfloat16> { static constexpr int TERMS = 3; };
+template <> struct Prob<__half> { static constexpr int TERMS = 2; };
+
 // Up to 16 query rows: keys stand on the M side of the products, S^T = K Q^T (16 keys x 8 rows a step) and O^T = V^T P^T (16 columns x 8
 // rows), so that eight rows - one token with a group of eight heads, a chain of seven - fill a tile that would be half empty with
 // the queries on that side: half the tensor instructions and half the accumulators.  Every warp has 16 keys of a tile to itself.
@@ -347,16 +355,21 @@ template <typename T, int HD, int ROWS> struct Narrow {
             __syncwarp();
         }
         // P^T as the products' second operand: two neighbouring rows of a key are packed and the 8 x 8 blocks transposed
-        uint32_t ph[N8][2], pl[N8][2];
+        constexpr int TERMS = Prob<T>::TERMS;
+        uint32_t p[TERMS][N8][2];
 #pragma unroll
         for (int n = 0; n < N8; ++n)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const float u = s[n][half * 2], v = s[n][half * 2 + 1];
-                const uint32_t hi = Num<T>::pack(u, v);
-                const float2 x = Num<T>::unpack(hi);
-                ph[n][half] = transposed(hi);
-                pl[n][half] = transposed(Num<T>::pack(u - x.x, v - x.y));
+                float u = s[n][half * 2], v = s[n][half * 2 + 1];
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    const uint32_t w = Num<T>::pack(u, v);
+                    const float2 x = Num<T>::unpack(w);
+                    p[k][n][half] = transposed(w);
+                    u -= x.x;
+                    v -= x.y;
+                }
             }
         constexpr int STEP = HD / 16 < 8 ? HD / 16 : 8;   // columns' products in flight
 #pragma unroll
@@ -367,9 +380,9 @@ template <typename T, int HD, int ROWS> struct Narrow {
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
 #pragma unroll
-                for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], ph[n][0], ph[n][1]);
+                for (int k = 0; k < TERMS; ++k)
 #pragma unroll
-                for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], pl[n][0], pl[n][1]);
+                    for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], p[k][n][0], p[k][n][1]);
             }
         }
     }
@@ -551,22 +564,28 @@ template <typename T, int HD, int ROWS> struct Wide {
         }
 #pragma unroll
         for (int ks = 0; ks < WK / 16; ++ks) {
-            uint32_t ph[4], pl[4];
+            constexpr int TERMS = Prob<T>::TERMS;
+            uint32_t p[TERMS][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float u = s[2 * ks + (e >> 1)][(e & 1) * 2], v = s[2 * ks + (e >> 1)][(e & 1) * 2 + 1];
-                ph[e] = Num<T>::pack(u, v);
-                const float2 h = Num<T>::unpack(ph[e]);
-                pl[e] = Num<T>::pack(u - h.x, v - h.y);
+                float u = s[2 * ks + (e >> 1)][(e & 1) * 2], v = s[2 * ks + (e >> 1)][(e & 1) * 2 + 1];
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    p[k][e] = Num<T>::pack(u, v);
+                    const float2 x = Num<T>::unpack(p[k][e]);
+                    u -= x.x;
+                    v -= x.y;
+                }
             }
 #pragma unroll
             for (int n = 0; n < HD / 8; n += 2) {
                 uint32_t vb[4];
                 ldsm4t(vb, (at_v ^ (n << 4)) + ks * 16 * HD * 2);
-                mma<T>(o[n], ph, vb[0], vb[1]);
-                mma<T>(o[n + 1], ph, vb[2], vb[3]);
-                mma<T>(o[n], pl, vb[0], vb[1]);
-                mma<T>(o[n + 1], pl, vb[2], vb[3]);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    mma<T>(o[n], p[k], vb[0], vb[1]);
+                    mma<T>(o[n + 1], p[k], vb[2], vb[3]);
+                }
             }
         }
     }
