@@ -376,7 +376,7 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* call, void
  * everything else is left alone.  max_len bounds the lengths, and so does what a table row can hold (a longer one is cut to it and flagged MTAD_ST_KV_OVERFLOW, a slot whose
  * table entry names no page is taken as zeros and flagged MTAD_ST_RANGE) and sizes the launch and the workspace.
  * Scores, sums and statistics are fp32; probabilities enter the product with the values as three bf16 or two fp16 terms (24 or 22
- * bits); the output is rounded once.  Results do not change from call to call.
+ * bits; in fp16 none below 2^-37 of the row's largest); the output is rounded once.  Results do not change from call to call.
  * The workspace (256-byte aligned) holds nothing between calls. */
 typedef struct mtad_paged_attn {
     const int32_t *lens, *n_rows;       /* device [batch]; n_rows may be NULL */

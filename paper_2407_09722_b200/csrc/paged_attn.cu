@@ -147,7 +147,7 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 constexpr float LN2 = 0.6931471805599453f;
-// of a row's sum: 0 for a row that sees nothing (its output is zero), NaN stays NaN
+// of a row's sum (times what the output is scaled by): 0 for a row that sees nothing (its output is zero), NaN stays NaN
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -211,17 +211,26 @@ __device__ __forceinline__ void zero_mixed(const AttnArgs& a, const TileAt& t, i
                 asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(t.v + at<HD>(first + r, c)), "r"(0u) : "memory");
 }
 
-// The reference of a row's exponentials is raised only when a score passes it by 2^RAISE: sums and outputs stay far inside fp32's range,
-// and most tiles need neither a maximum over lanes nor a rescaling.
-constexpr float RAISE = 6.f;
-
 // Terms of the cache's type as which a probability enters the second product: three of bf16 hold the 24 bits of fp32, two of fp16 hold 22.
 // (Two of bf16 left 2^-18 of a probability out, which turned the rounding of one output in 2000.  The third takes no time where memory bounds
 // the call, up to 16 query rows a KV head; a chain of 5 on groups of 8, eight ragged sequences, takes 42.8 us instead of 37.9, four prompt
 // chunks of 256 rows at 2000 to 4000 slots 588 instead of 498.)
+//
+// The reference of a row's exponentials is raised only when a score passes it by 2^RAISE: sums and outputs stay far inside fp32's range,
+// and most tiles need neither a maximum over lanes nor a rescaling.
+//
+// fp16 has no steps below 2^-24: a probability enters (and the output is kept) times SCALE, so that the largest, 2^RAISE * SCALE, is just below
+// the type's end and the steps are 2^-37 of the reference.  (As it is, 2^-25 and less vanished from the output, and many slots behind a
+// dominant one with them.  A lower RAISE than that of bf16 for two bits more: 60 to 61 us for the ragged batch in fp16 either way.)
 template <typename T> struct Prob;
-template <> struct Prob<__nv_bfloat16> { static constexpr int TERMS = 3; };
-template <> struct Prob<__half> { static constexpr int TERMS = 2; };
+template <> struct Prob<__nv_bfloat16> {
+    static constexpr int TERMS = 3;
+    static constexpr float RAISE = 6.f, SCALE = 1.f;
+};
+template <> struct Prob<__half> {
+    static constexpr int TERMS = 2;
+    static constexpr float RAISE = 2.f, SCALE = 8192.f;
+};
 
 // Up to 16 query rows: keys stand on the M side of the products, S^T = K Q^T (16 keys x 8 rows a step) and O^T = V^T P^T (16 columns x 8
 // rows), so that eight rows - one token with a group of eight heads, a chain of seven - fill a tile that would be half empty with
@@ -311,7 +320,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
                     for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
                     const float to = fmaxf(m[n][e], x), f = m[n][e] == to ? 1.f : ex2(m[n][e] - to);
                     m[n][e] = to;
-                    over[n][e] = to + RAISE;
+                    over[n][e] = to + Prob<T>::RAISE;
                     ref[n][e] = to == -CUDART_INF_F ? 0.f : to;
                     l[n][e] *= f;
 #pragma unroll
@@ -338,7 +347,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
                     for (int n = 0; n < N8; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float pr = __shfl_sync(0xffffffffu, s[n][half * 2 + e], (kk << 2) | (lane & 3));
+                            const float pr = __shfl_sync(0xffffffffu, s[n][half * 2 + e], (kk << 2) | (lane & 3)) * Prob<T>::SCALE;
                             if (sees(a, j, pos[n][e]))
 #pragma unroll
                                 for (int d = 0; d < HD / 16; ++d)
@@ -361,7 +370,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
         for (int n = 0; n < N8; ++n)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                float u = s[n][half * 2], v = s[n][half * 2 + 1];
+                float u = s[n][half * 2] * Prob<T>::SCALE, v = s[n][half * 2 + 1] * Prob<T>::SCALE;
 #pragma unroll
                 for (int k = 0; k < TERMS; ++k) {
                     const uint32_t w = Num<T>::pack(u, v);
@@ -517,7 +526,7 @@ template <typename T, int HD, int ROWS> struct Wide {
                 if (pos_b >= 0) *reinterpret_cast<float2*>(row + 8 * a.score_ld + n * 8) = make_float2(s[n][2], s[n][3]);
             }
         }
-        if (__any_sync(0xffffffffu, x_a > m_a + RAISE || x_b > m_b + RAISE)) {
+        if (__any_sync(0xffffffffu, x_a > m_a + Prob<T>::RAISE || x_b > m_b + Prob<T>::RAISE)) {
 #pragma unroll
             for (int d = 1; d < 4; d <<= 1) {
                 x_a = fmaxf(x_a, __shfl_xor_sync(0xffffffffu, x_a, d));
@@ -546,8 +555,8 @@ template <typename T, int HD, int ROWS> struct Wide {
                     const int kk = wk * WK + k8 * 8 + e, j = t.j0 + kk;
                     if (!mixed(a, t, j)) continue;
                     const int from = (lane & ~3) | (e >> 1);
-                    const float p_a = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][1] : s[k8][0], from);
-                    const float p_b = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][3] : s[k8][2], from);
+                    const float p_a = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][1] : s[k8][0], from) * Prob<T>::SCALE;
+                    const float p_b = __shfl_sync(0xffffffffu, (e & 1) ? s[k8][3] : s[k8][2], from) * Prob<T>::SCALE;
                     const bool see_a = sees(a, j, pos_a), see_b = sees(a, j, pos_b);
 #pragma unroll
                     for (int n = 0; n < HD / 8; ++n) {
@@ -568,7 +577,7 @@ template <typename T, int HD, int ROWS> struct Wide {
             uint32_t p[TERMS][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float u = s[2 * ks + (e >> 1)][(e & 1) * 2], v = s[2 * ks + (e >> 1)][(e & 1) * 2 + 1];
+                float u = s[2 * ks + (e >> 1)][(e & 1) * 2] * Prob<T>::SCALE, v = s[2 * ks + (e >> 1)][(e & 1) * 2 + 1] * Prob<T>::SCALE;
 #pragma unroll
                 for (int k = 0; k < TERMS; ++k) {
                     p[k][e] = Num<T>::pack(u, v);
@@ -888,7 +897,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
                         if (d == 0) a.part_ml[place * ROWS + m] = ml;
                     } else {
                         const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-                        const float inv = inverse(ml.y);
+                        const float inv = inverse(ml.y * Prob<T>::SCALE);
                         if (d < a.kv.hd)
                             *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
                                 make_uint2(Num<T>::pack(x.x * inv, x.y * inv), Num<T>::pack(x.z * inv, x.w * inv));
@@ -958,7 +967,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
                     acc.x += f * x[k].x; acc.y += f * x[k].y; acc.z += f * x[k].z; acc.w += f * x[k].w;
                 }
             const int r = (m0 + m) / a.G, hq = h * a.G + (m0 + m) - r * a.G;
-            const float inv = inverse(sum);
+            const float inv = inverse(sum * Prob<T>::SCALE);
             *reinterpret_cast<uint2*>(a.out + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + d) =
                 make_uint2(Num<T>::pack(acc.x * inv, acc.y * inv), Num<T>::pack(acc.z * inv, acc.w * inv));
             if (d == 0 && a.lse) a.lse[((long long)C.b * a.R + r) * (a.kv.Hkv * a.G) + hq] = (mx + log2f(sum)) * LN2;
@@ -1133,7 +1142,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) stream_kernel(cons
                 } else {
                     const int r = m / a.G, hq = C.hr * a.G + m - r * a.G;
                     T* dst = reinterpret_cast<T*>(a.out) + (long long)C.b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + core.g;
-                    const float inv = inverse(core.l[n][e]);
+                    const float inv = inverse(core.l[n][e] * Prob<T>::SCALE);
 #pragma unroll
                     for (int d = 0; d < HD / 16; ++d) {
                         if (d * 16 < a.kv.hd) dst[d * 16] = Num<T>::from(core.o[d][n][e] * inv);
@@ -1263,7 +1272,7 @@ __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_joi
                 for (int k = 0; k < PER; ++k) acc[k] += s_acc[w][lane * PER + k];
         }
         const int r = row / a.G, hq = h * a.G + row - r * a.G;
-        const float inv = inverse(ml.y);
+        const float inv = inverse(ml.y * Prob<T>::SCALE);
         if (lane * PER < a.kv.hd) {
             uint16_t* dst = a.out + (long long)b * a.o_sb + (long long)r * a.o_sr + (long long)hq * a.o_sh + lane * PER;
 #pragma unroll

@@ -57,3 +57,46 @@ def test_attention_probabilities_keep_their_bits(dtype, group, most):
     want = ((p - h.double() - l.double()) / (2 + p))[:, None, None, None]
     assert bool(((out.double() - want).abs() <= half_step(dt) * want.abs() + 2.0 ** -21 * (p / (2 + p))[:, None, None, None] +
                  torch.finfo(dt).smallest_normal * torch.finfo(dt).eps).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("group", [1, 16, 20, 40])
+@pytest.mark.parametrize("n,most", [(700, 700), (30000, 30000)])
+def test_attention_many_slots_far_below_one(dtype, group, n, most):
+    """The first slot has a score 17.5 above all others (what an attention sink looks like) and the value 0; the others' probabilities, 2^-25.2 each,
+    make the output.  Their exponent 25.2 is off by two roundings (2^-24 of it each, 2^-18.9 of a probability); exponentials and sums of n
+    terms of one size, in chains of at most n / 16 with the lanes' and tiles' in between, by 2^-16 with room; in fp16 a probability is a multiple of
+    2^-37 of the largest, off by half of that: 2^-12.8 of 2^-25.2.  The output is then rounded once."""
+    dt = DT[dtype]
+    hd = 64
+    k, v = torch.zeros(1, n, 1, hd, dtype=dt, device="cuda"), torch.ones(1, n, 1, hd, dtype=dt, device="cuda")
+    k[:, 0, 0, 3], v[:, 0] = 1, 0
+    v[:, :, 0, 1::2] *= -0.5
+    q = torch.zeros(1, 1, group, hd, dtype=dt, device="cuda")
+    q[..., 3] = 17.5
+    kp, vp, table = small_cache(k, v, 16, 0)
+    out, lse = M.paged_attention(q, kp, vp, table, torch.full((1,), n, dtype=torch.int32, device="cuda"), scale=1.0, max_len=most, return_lse=True)
+    p = math.exp(-17.5)
+    want = torch.tensor([1.0, -0.5], dtype=torch.float64, device="cuda").repeat(hd // 2) * ((n - 1) * p / (1 + (n - 1) * p))
+    near = 2.0 ** -18.9 + 2.0 ** -16 + (2.0 ** -38 / p if dtype == "fp16" else 0.0)
+    assert bool(((out.double() - want).abs() <= (half_step(dt) + near) * want.abs() + torch.finfo(dt).smallest_normal * torch.finfo(dt).eps).all())
+    assert bool(((lse.double() - 17.5 - math.log1p((n - 1) * p)).abs() <= 17.5 * 2.0 ** -22 + 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("rows,group", [(3, 2), (3, 4), (9, 2), (9, 4)])
+@pytest.mark.parametrize("most", [64, 4096])
+def test_attention_fp16_values_added_by_hand(rows, group, most):
+    """An infinite value that only the last row sees: that value's row is added outside the products.  Every other output is what it
+    was, but for the order of fp32 sums (2^-20 of the largest value with room) and a rounding each."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.empty(2, 50, 2, 64, dtype=torch.float16, device="cuda").normal_(generator=g) for _ in range(2))
+    q = torch.empty(2, rows, 2 * group, 64, dtype=torch.float16, device="cuda").normal_(generator=g)
+    lens = torch.full((2,), 50, dtype=torch.int32, device="cuda")
+    kp, vp, table = small_cache(k, v, 16, most // 16)
+    want = M.paged_attention(q, kp, vp, table, lens, max_len=most).double()
+    v[1, 49, :, 7] = float("inf")
+    kp, vp, table = small_cache(k, v, 16, most // 16)
+    got = M.paged_attention(q, kp, vp, table, lens, max_len=most).double()
+    assert bool((got[1, rows - 1, :, 7] == float("inf")).all())
+    got[1, rows - 1, :, 7] = want[1, rows - 1, :, 7]
+    assert bool(((got - want).abs() <= 2 * half_step(torch.float16) * want.abs() + 2.0 ** -20 * float(v[v.isfinite()].abs().max())).all())
