@@ -391,7 +391,7 @@ typedef struct mtad_paged_attn {
     int32_t batch, rows, n_q_heads;     /* rows <= MTAD_MAX_NODES + 1 */
     int32_t window, sinks;              /* window 0: every slot up to the row's own */
     int32_t max_len;
-    float scale;                        /* 0: 1 / sqrt(head_dim) */
+    float scale;                        /* 0: 1 / sqrt(head_dim); else finite, of either sign */
 } mtad_paged_attn;
 int mtad_paged_attention_workspace(const mtad_paged_kv* kv, const mtad_paged_attn* call, size_t* out_bytes);
 int mtad_paged_attention(const mtad_paged_kv* kv, const mtad_paged_attn* call, void* workspace, size_t workspace_bytes, void* stream);

@@ -1383,7 +1383,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     if (!lie_apart(kv->head_dim, {{a.B, a.o_sb}, {a.R, a.o_sr}, {c->n_q_heads, a.o_sh}})) return MTAD_E_INVALID;
     if (c->weights && !lie_apart(a.max_len, {{a.B, c->weights_stride_seq}, {kv->n_kv_heads, c->weights_stride_head}})) return MTAD_E_INVALID;
     if (a.window >= a.max_len) a.window = a.sinks = 0;    // (every slot is inside it)
-    a.scale2 = (float)((c->scale > 0.f ? (double)c->scale : 1.0 / sqrt((double)kv->head_dim)) * 1.4426950408889634);
+    a.scale2 = (float)((c->scale != 0.f ? (double)c->scale : 1.0 / sqrt((double)kv->head_dim)) * 1.4426950408889634);
     a.weights = c->weights; a.w_sb = c->weights_stride_seq; a.w_sh = c->weights_stride_head;
     p->HD = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
     const int M = a.R * a.G;

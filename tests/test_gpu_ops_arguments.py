@@ -1,0 +1,27 @@
+"""Arguments of the operators around a decoder of the caller's own that the other tests leave at their defaults, and what a call leaves alone."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_09722_b200 as M
+from tests.test_gpu_ops import Cache, attention_ref, check_attention, half_step, queries
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("scale", [0.3, 1e-3, -0.25, -1.0])
+@pytest.mark.parametrize("rows,hq,most", [(1, 4, 700), (3, 16, 700), (5, 24, 700), (1, 4, 5000), (5, 24, 5000)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
+def test_attention_scale(scale, rows, hq, most, window, sinks):
+    """Any finite scale but 0, which stands for 1 / sqrt(head_dim): the sign is the caller's.  (A negative one is the positive one on
+    queries of the other sign, which the reference and its bound are taken from.)"""
+    c = Cache(15, [most, 64, 130], 2, 64, 16)
+    q = queries(15, 3, rows, hq, 64, torch.bfloat16)
+    if scale > 0:
+        check_attention(c, q, scale=scale, window=window, sinks=sinks)
+        return
+    ref, lse_ref, _, tol, tol_s = attention_ref(c, -q, [rows] * 3, window, sinks, -scale)
+    out, lse = M.paged_attention(q, *c.args(), c.lens, window=window, sinks=sinks, scale=scale, max_len=most, return_lse=True)
+    assert bool(((out.double() - ref).abs() <= half_step(q.dtype) * ref.abs() + tol + torch.finfo(q.dtype).smallest_normal).all())
+    assert bool(((lse.double() - lse_ref).abs() <= tol_s + 2.0 ** -21 * lse_ref.abs()).all())
