@@ -154,6 +154,8 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// of a slot for a row, from its score: none where the row does not see the slot (score -inf), also where its sum is NaN
+__device__ __forceinline__ float weight(float score, float lse) { return score == -CUDART_INF_F ? 0.f : ex2(score - lse); }
 
 // Byte offset of 16-byte piece c of row r of a tile: the pieces of eight neighbouring rows fall into different banks.  Tiles begin at
 // multiples of 512 bytes, so that the pieces 2 k, 2 k + 1 of a row lie at (address of the pieces 0, 1) ^ (k << 5).
@@ -993,7 +995,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
 #pragma unroll 4
                 for (int m = 0; m < rows; ++m) {
                     const float lse = s_lse[m];
-                    if (lse != -CUDART_INF_F) acc += ex2(z[(long long)m * a.score_ld + j] - lse);
+                    if (lse != -CUDART_INF_F) acc += weight(z[(long long)m * a.score_ld + j], lse);
                 }
                 dst[j] += acc;
             }
@@ -1329,7 +1331,7 @@ __global__ void __launch_bounds__(NT, 8) join_kernel(const AttnArgs a, int n_joi
                 if (m0 + m >= rows) break;
                 const float lse = s_lse[m0 + m];
                 if (lse == -CUDART_INF_F) continue;       // (a row that sees nothing has no scores)
-                acc[0] += ex2(x[m].x - lse); acc[1] += ex2(x[m].y - lse); acc[2] += ex2(x[m].z - lse); acc[3] += ex2(x[m].w - lse);
+                acc[0] += weight(x[m].x, lse); acc[1] += weight(x[m].y, lse); acc[2] += weight(x[m].z, lse); acc[3] += weight(x[m].w, lse);
             }
 #pragma unroll
             for (int m = 0; m < 8; ++m)
