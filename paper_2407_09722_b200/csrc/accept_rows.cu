@@ -11,7 +11,7 @@
 // exponentials (16 a clock and SM: 24 us of 64 sequences x 13 rows x 128000 bf16 logits whose bytes take 33), at small
 // batches by latency.  A cluster of four or eight blocks has a sequence, a block its part of the vocabulary; warps take (row, part) tasks, a
 // reference and a sum a lane; rows' statistics and the draw's candidates cross the cluster in distributed shared memory, so
-// the call is one launch and needs no workspace.  Statistics are fp32, merged in a fixed order.  The batch of 64 takes 60 us (4.1 TB/s;
+// the call is one launch and needs no workspace.  Statistics are fp32, merged in a fixed order.  The batch of 64 takes 61 us (4.0 TB/s;
 // 14 of them the draw, whose loads wait for the accepted prefix), one chain of 5 rows of 32000 fp32 logits 11 us.
 #include <cooperative_groups.h>
 #include <math.h>
@@ -26,20 +26,22 @@ namespace mtad {
 namespace {
 
 constexpr int AC_ROWS = 2 * MTAD_MAX_DEPTH + 1, AC_PARTS = 8;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LN2 = 0.6931471805599453f;
 
 struct AcceptRowsArgs {
     const void *z, *q;               // target rows [B, gamma + 1, V], auxiliary rows [B, gamma, V] or null (threshold rule)
     long long z_sb, z_sr, q_sb, q_sr;
     const int32_t *tok, *n_draft;
     const float *draft_logq, *u_accept, *u_last;
-    float z_mul, q_mul, log_tau;     // 1 / temperature
+    float z_mul, q_mul, log_tau;     // log2(e) / temperature
+    double z_unit;                   // 1 / temperature over z_mul as it is: from powers of two back to the rows' own logarithms
     int gamma, V;
     mtad_result out;
 };
 
-// Statistics of logits over the temperature, in powers of two: x = z * c, c = log2(e) / temperature.  The reference is a whole number not
-// below the largest x, so x - ref is one fused multiply-add whose only rounding is the result's: no bias enters a sum of many.
+// Statistics of logits over the temperature, in powers of two: x = z * c, c = log2(e) / temperature.  The reference is a whole number, so
+// x - ref is one fused multiply-add whose only rounding is the result's: no bias enters a sum of many.  Reference and sum stay apart to the
+// end: whatever has been added to a row is in the reference alone, and a log-probability, (x - ref) - log2(sum), does not see it.
 struct Stat {
     float m, s;                      // reference, sum of 2^(x - m)
 };
@@ -47,6 +49,15 @@ __device__ __forceinline__ float ex2a(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// The sum within [1/2, 1): log2(sum) is small beside x - ref
+__device__ __forceinline__ Stat settled(Stat a) {
+    if (fabsf(a.m) < 0x1p23f) {                           // (references beyond are no longer whole numbers apart)
+        int k = 0;
+        a.s = frexpf(a.s, &k);
+        a.m += (float)k;
+    }
+    return a;
 }
 __device__ __forceinline__ Stat merge(const Stat& a, const Stat& b) {
     const float m = fmaxf(a.m, b.m);
@@ -219,7 +230,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
     __shared__ Stat s_part[AC_ROWS * AC_PARTS];
     __shared__ Stat s_row[AC_ROWS];                       // read by the cluster
     __shared__ Best s_best[WARPS], s_block;            // s_block: read by the cluster
-    __shared__ float s_lse[AC_ROWS];
+    __shared__ float s_ref[AC_ROWS], s_sum[AC_ROWS], s_log[AC_ROWS];      // of a row: the reference, the sum, its logarithm
     __shared__ int s_eta;
     const int D = a.gamma, V = a.V;
     pdl_wait();
@@ -240,8 +251,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
             x = __ldg(a.tok + (long long)b * D + lane);
             bad = (unsigned)x >= (unsigned)V;
             if (!bad) {
-                zx = Row<T>::one(z[(long long)lane * a.z_sr + x]) * a.z_mul;
-                if (spd) qx = Row<T>::one(q[(long long)lane * a.q_sr + x]) * a.q_mul;
+                zx = Row<T>::one(z[(long long)lane * a.z_sr + x]);
+                if (spd) qx = Row<T>::one(q[(long long)lane * a.q_sr + x]);
             }
         }
         if (__any_sync(0xffffffffu, bad)) bits |= MTAD_ST_BAD_TOKEN;
@@ -264,8 +275,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
     const int step = ((v1 - v0 + parts - 1) / parts + Row<T>::N - 1) / Row<T>::N * Row<T>::N;
     for (int t = warp; t < rows * parts; t += WARPS) {
         const int r = t / parts, p = t - r * parts, e0 = min(v0 + p * step, v1), e1 = min(e0 + step, v1);
-        const Stat st = r <= g ? row_stat<T>(z + (long long)r * a.z_sr, e0, e1, a.z_mul * LOG2E, lane)
-                               : row_stat<T>(q + (long long)(r - g - 1) * a.q_sr, e0, e1, a.q_mul * LOG2E, lane);
+        const Stat st = r <= g ? row_stat<T>(z + (long long)r * a.z_sr, e0, e1, a.z_mul, lane)
+                               : row_stat<T>(q + (long long)(r - g - 1) * a.q_sr, e0, e1, a.q_mul, lane);
         if (lane == 0) s_part[t] = st;
     }
     __syncthreads();
@@ -278,20 +289,25 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
     if (tid < rows) {
         Stat st = *cluster.map_shared_rank(&s_row[tid], 0);
         for (int k = 1; k < CLUSTER; ++k) st = merge(st, *cluster.map_shared_rank(&s_row[tid], k));
-        s_lse[tid] = (st.m + log2f(st.s)) * LN2;
+        st = settled(st);
+        s_ref[tid] = st.m;
+        s_sum[tid] = st.s;
+        s_log[tid] = log2f(st.s);
     }
     __syncthreads();
+    // of a logit of row r (a product by itself: fused into a difference of two, equal ones would no longer cancel)
+    auto log_p = [&](float x, float c, int r) { return __fmul_rn(fmaf(x, c, -s_ref[r]) - s_log[r], LN2); };
     // ---- the accepted prefix (warp 0 of every block; the first block writes)
     if (warp == 0) {
         const bool w = rank == 0;
         bool finite = true;
-        for (int r = lane; r < rows; r += 32) finite = finite && isfinite(s_lse[r]);
+        for (int r = lane; r < rows; r += 32) finite = finite && isfinite(s_ref[r]) && isfinite(s_log[r]);
         if (!__all_sync(0xffffffffu, finite)) bits |= MTAD_ST_NONFINITE;
-        const float lp = lane < g ? zx - s_lse[lane] : 0.f;
+        const float lp = lane < g ? log_p(zx, a.z_mul, lane) : 0.f;
         int eta = 0;
         float gap = CUDART_INF_F, LP = lp;
         if (spd) {
-            const float ratio = lane < g ? fminf(0.f, lp - (qx - s_lse[g + 1 + lane])) : 0.f;   // (NaN, 0 over 0: rejected, below)
+            const float ratio = lane < g ? fminf(0.f, lp - log_p(qx, a.q_mul, g + 1 + lane)) : 0.f;   // (NaN, 0 over 0: rejected, below)
             const float lu = lane < g ? logf(__ldg(a.u_accept + (long long)b * D + lane)) : 0.f;
             const bool ok = lane < g && lp > -CUDART_INF_F && lu < ratio;
             const uint32_t no = __ballot_sync(0xffffffffu, !ok);
@@ -331,7 +347,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
                 }
                 if (lane < g && o.node_lp) o.node_lp[(long long)b * D + lane] = lp;
                 if (lane < g && o.node_LP && !spd) o.node_LP[(long long)b * D + lane] = LP;
-                if (o.row_lse) for (int r = lane; r <= g; r += 32) o.row_lse[(long long)b * (D + 1) + r] = s_lse[r];
+                if (o.row_lse)
+                    for (int r = lane; r <= g; r += 32) o.row_lse[(long long)b * (D + 1) + r] = (float)(((double)s_ref[r] + (double)s_log[r]) * a.z_unit);
             }
         }
     }
@@ -343,12 +360,12 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
     auto search = [&](bool rest) {
         const T* row = z + (long long)eta * a.z_sr;
         const T* qrow = rest ? q + (long long)eta * a.q_sr : row;
-        const float cz = a.z_mul * LOG2E, cq = a.q_mul * LOG2E;
-        const float rz = s_lse[eta] * LOG2E, rq = rest ? s_lse[g + 1 + eta] * LOG2E : 0.f;
+        const float cz = a.z_mul, cq = a.q_mul, rz = s_ref[eta], rq = rest ? s_ref[g + 1 + eta] : 0.f;
+        const float k = rest ? s_sum[eta] / s_sum[g + 1 + eta] : 0.f;      // (p - q) * sum of p's row: one factor, 1 where the rows are the same
         const float* u = a.u_last + (long long)b * V;
         float lead = 0.f;                                 // the best that this warp has seen
         auto look = [&](float x, float y, float un, int v) {
-            const float w = ex2a(fmaf(x, cz, -rz)) - ex2a(fmaf(y, cq, -rq));
+            const float w = fmaf(-k, ex2a(fmaf(y, cq, -rq)), ex2a(fmaf(x, cz, -rz)));
             if (w > 0.f && !(w < lead * (1.f - un))) better(best, w / -logf(un), v);
         };
         auto share = [&]() { lead = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(best.y, 0.f)))); };
@@ -424,7 +441,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS, 1024 
         if (rank == 0 && tid == 0) {
             const int t = best.v != 0x7fffffff ? best.v : 0;
             a.out.out_tok[(long long)b * (D + 1) + eta] = t;
-            a.out.out_lp[(long long)b * (D + 1) + eta] = Row<T>::one(z[(long long)eta * a.z_sr + t]) * a.z_mul - s_lse[eta];
+            a.out.out_lp[(long long)b * (D + 1) + eta] = log_p(Row<T>::one(z[(long long)eta * a.z_sr + t]), a.z_mul, eta);
         }
     }
     cluster.sync();                                       // (no block leaves while another reads its shared memory)
@@ -446,7 +463,9 @@ int accept_rows(const mtad_accept_rows* c, const float* draft_logq, float log_ta
     a.z_sb = c->logits_stride_seq; a.z_sr = c->logits_stride_row; a.q_sb = c->draft_stride_seq; a.q_sr = c->draft_stride_row;
     a.tok = c->draft_tok; a.n_draft = c->n_draft;
     a.draft_logq = draft_logq; a.u_accept = u_accept; a.u_last = c->last_uniform;
-    a.z_mul = 1.f / c->temperature; a.q_mul = q ? 1.f / c->draft_temperature : 1.f; a.log_tau = log_tau;
+    a.z_mul = (float)(1.4426950408889634 / c->temperature); a.q_mul = q ? (float)(1.4426950408889634 / c->draft_temperature) : 1.f;
+    a.z_unit = 1.0 / c->temperature / a.z_mul;
+    a.log_tau = log_tau;
     a.gamma = c->gamma; a.V = c->vocab;
     a.out = *out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -100,3 +100,69 @@ def test_attention_fp16_values_added_by_hand(rows, group, most):
     assert bool((got[1, rows - 1, :, 7] == float("inf")).all())
     got[1, rows - 1, :, 7] = want[1, rows - 1, :, 7]
     assert bool(((got - want).abs() <= 2 * half_step(torch.float16) * want.abs() + 2.0 ** -20 * float(v[v.isfinite()].abs().max())).all())
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# accept rules.  A log-probability is the difference of a logit and the row's largest (one rounding, 2^-24 of it) less the logarithm of a
+# sum: its terms are off by 2^-20.5 (an exponent up to 32 in fp32, the exponential), the sum of at most 2^7 in a chain by 2^-19 at the very
+# worst and by 2^-21 as terms round, the logarithm by 2^-22.  2^-19 and 2^-22 of the value hold all of it.
+
+def lp_bound(lp):
+    return 2.0 ** -19 + 2.0 ** -22 * lp.abs()
+
+
+def accept_both(z, dr, tok, u, ua, temperature=1.0):
+    B, D = tok.shape
+    got = []
+    for rule in ("mtad", "spd"):
+        res = M.ResultBuffers(B, D, D)
+        if rule == "spd":
+            M.accept_chain_spd(z, tok, dr, ua, u, res, temperature=temperature, draft_temperature=temperature)
+        else:
+            logq = torch.log_softmax(dr.double() / temperature, -1).gather(2, tok.long()[..., None])[..., 0].cumsum(-1).float()
+            M.accept_chain(z, tok, logq, math.log(0.2), u, res, temperature=temperature)
+        assert not res.status.any()
+        got.append({n: getattr(res, n).clone() for n in ("eta", "n_out", "out_tok", "out_lp", "node_lp", "row_lse")})
+    return got
+
+
+def check_accept_lp(z, tok, got, temperature=1.0):
+    B, D = tok.shape
+    lse = torch.logsumexp(z.double() / temperature, -1)
+    lp = z.double() / temperature - lse[..., None]
+    want = lp[:, :D].gather(2, tok.long()[..., None])[..., 0]
+    b = torch.arange(B, device="cuda")
+    for r in got:
+        assert bool(((r["node_lp"].double() - want).abs() <= lp_bound(want)).all()), float((r["node_lp"].double() - want).abs().max())
+        assert bool(((r["row_lse"].double() - lse).abs() <= 2.0 ** -24 * lse.abs() + 2.0 ** -19).all()), float((r["row_lse"].double() - lse).abs().max())
+        last = lp[b, r["eta"].long(), r["out_tok"][b, r["eta"].long()].long()]
+        assert bool(((r["out_lp"][b, r["eta"].long()].double() - last).abs() <= lp_bound(last)).all())
+
+
+def accept_inputs(seed, B, D, V, step, top):
+    """Target rows that are multiples of `step` below `top` in magnitude, the auxiliary model's near them."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = ((torch.randn(B, D + 1, V, device="cuda", generator=g) * 2).clamp_(-top, top) / step).round() * step
+    dr = ((z[:, :D] + torch.randn(B, D, V, device="cuda", generator=g)).clamp_(-top, top) / step).round() * step
+    tok = torch.randint(0, V, (B, D), device="cuda", generator=g, dtype=torch.int32)
+    tok[:, 0] = z[:, 0].argmax(-1).int()
+    u, ua = (torch.rand(*d, device="cuda", generator=g).clamp_(2.0 ** -24, 1 - 2.0 ** -24) for d in ((B, V), (B, D)))
+    return z, dr, tok, u, ua
+
+
+@pytest.mark.parametrize("dtype,step,top,constant", [("fp32", 2.0 ** -10, 8, 8192 - 16), ("fp32", 2.0 ** -10, 8, -8192 + 16), ("bf16", 1.0, 8, 192), ("fp16", 0.5, 8, -960),
+                                                     ("fp32", 2.0 ** -2, 8, 3000000.0)])
+@pytest.mark.parametrize("temperature", [1.0, 0.6875])
+def test_accept_rows_with_a_constant_added(dtype, step, top, constant, temperature):
+    """Any constant may have been added to a row (here one that leaves every logit exact): log-probabilities, decisions and draws are
+    those of the row without it, to the same bound, and only the log-sum-exp moves."""
+    z, dr, tok, u, ua = accept_inputs(3, 6, 4, 1500, step, top)
+    z, dr, far = z.to(DT[dtype]), dr.to(DT[dtype]), (z + constant).to(DT[dtype])
+    assert torch.equal(far.double() - constant, z.double()) and torch.equal((dr.float() - constant).to(DT[dtype]).double() + constant, dr.double())
+    here = accept_both(z, dr, tok, u, ua, temperature)
+    there = accept_both(far, (dr.float() - constant).to(DT[dtype]), tok, u, ua, temperature)
+    check_accept_lp(z, tok, here, temperature)
+    check_accept_lp(far, tok, there, temperature)
+    for a, b in zip(here, there):
+        for n in ("eta", "n_out", "out_tok"):
+            assert torch.equal(a[n], b[n])
