@@ -373,7 +373,8 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* call, void
  * A row that sees nothing (length 0, or at < 0) gives zeros and lse -inf.  Infinities and NaN in slots that a row does not
  * see do not reach it.  Rows beyond n_rows[b] are left as they were.  weights, if given, accumulates what mtad_paged_evict
  * selects by: weights[b][kv head][j] += the sum of p_j over the sequence's rows and the heads of the group, for visible j;
- * everything else is left alone.  max_len bounds the lengths, and so does what a table row can hold (a longer one is cut to it and flagged MTAD_ST_KV_OVERFLOW, a slot whose
+ * everything else is left alone: columns of slots that become free (rows that were not accepted, slots behind an eviction) are the caller's
+ * to clear before other tokens take the slots.  max_len bounds the lengths, and so does what a table row can hold (a longer one is cut to it and flagged MTAD_ST_KV_OVERFLOW, a slot whose
  * table entry names no page is taken as zeros and flagged MTAD_ST_RANGE) and sizes the launch and the workspace.
  * Scores, sums and statistics are fp32; probabilities enter the product with the values as three bf16 or two fp16 terms (24 or 22
  * bits; in fp16 none below 2^-37 of the row's largest); the output is rounded once.  Results do not change from call to call.
@@ -399,7 +400,8 @@ int mtad_paged_attention(const mtad_paged_kv* kv, const mtad_paged_attn* call, v
 /* Eviction, per sequence and KV head.  Where lens[b] > keep, the first `first` slots, the last `recent` ones and of the rest those
  * with the largest scores stay, keep in all (first + recent <= keep; equal scores: the lower slot; NaN counts as larger than
  * every number).  They move to slots 0 .. keep - 1 in the order of their slots, so that the last tokens stay the last; slots from keep
- * on are left as they were.  kept[b][h][i] is the former slot of slot i (-1 from the new length on), scores_out[b][h][i] its score;
+ * on are left as they were.  kept[b][h][i] is the former slot of slot i (-1 from the new length on), scores_out[b][h][i] its score
+ * (columns from the new length on are left as they were);
  * scores_out may be scores itself for max_len up to 327680 (MTAD_E_UNIMPLEMENTED beyond; a zero then loses its sign and a NaN its
  * bits).  new_lens[b] = min(lens[b], keep); it
  * must not be lens.  The pages of a sequence that is longer than keep must be its own: no other table row, nor another place

@@ -3,7 +3,8 @@ mtad_accept_chain and mtad_accept_chain_spd (see include/mtad.h for what each co
 
 They take torch tensors, allocate what is not handed in (outputs, scratch) from torch's allocator on the stream they run on, and
 enqueue on the current stream of the tensors' device unless `stream` says otherwise.  Argument errors raise MtadError with the library's
-code, or ValueError where a tensor has the wrong device, type or layout.  The marshalling is compiled (csrc/ops_py.cpp).
+code, or ValueError where a tensor has the wrong device, type or layout.  They have no backward pass: inputs that require a gradient are
+read, outputs do not.  The marshalling is compiled (csrc/ops_py.cpp).
 """
 from __future__ import annotations
 
@@ -55,7 +56,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
                     lse: Optional[torch.Tensor] = None, return_lse: bool = False, max_len: Optional[int] = None,
                     status: Optional[torch.Tensor] = None, stream=None):
     """Attention of the last rows of every sequence, q [sequences, rows, heads, head_dim], over its slots.  `weights` [sequences, kv
-    heads, slots] fp32 accumulates the attention that each slot drew.  `max_len` (default: all that the table can hold) bounds
+    heads, slots] fp32 accumulates the attention that each slot drew (clear what lies behind a length that went down, before other
+    tokens take those slots).  `max_len` (default: all that the table can hold) bounds
     the lengths: the tighter, the less scratch and the better the launch fits.  Returns the output, with return_lse also the
     log of the softmax sums [sequences, rows, heads]."""
     r = (_mod or _ops()).attention(q, k_pages, v_pages, table, lens, n_rows, window, sinks, scale, weights, out, lse, return_lse, max_len,
@@ -70,7 +72,8 @@ def paged_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tenso
                 scores_out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, status: Optional[torch.Tensor] = None,
                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Cuts sequences longer than `keep` back to the first, the last and the best-scored slots of every KV head; returns the former
-    slots [sequences, kv heads, keep] and the new lengths."""
+    slots [sequences, kv heads, keep] and the new lengths.  `scores_out`, which may be `scores`, gets the scores of what stays; its columns
+    from the new lengths on are left as they were (of accumulated weights: clear them)."""
     r = (_mod or _ops()).evict(k_pages, v_pages, table, lens, scores, keep, first, recent, kept, new_lens, scores_out, max_len, status,
                                None if stream is None else _handle(stream))
     if type(r) is int:
