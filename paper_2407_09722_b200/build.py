@@ -48,8 +48,10 @@ def build_ops(verbose: bool = False) -> str:
     for d in (os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
               sysconfig.get_paths()["include"], "/usr/local/cuda/include"):
         cmd += ["-I", d]
+    # (libstdc++ by name, ahead of the compiler's own: one that comes with the archive only would put a second copy of it into the module, and
+    # a number written to a stream of torch's then ends the process)
     cmd += [OPS_SRC, "-o", OPS, "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
-            "-L", HERE, "-l:libmtad.so", "-Wl,-rpath,$ORIGIN"]
+            "-L", HERE, "-l:libmtad.so", "-l:libstdc++.so.6", "-Wl,-rpath,$ORIGIN"]
     if verbose:
         print(" ".join(cmd))
     subprocess.run(cmd, check=True)

@@ -9,7 +9,6 @@
 
 #include <algorithm>
 #include <optional>
-#include <string>
 
 #include "mtad.h"
 
@@ -34,12 +33,6 @@ float real(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw python_error();
     return (float)v;
-}
-// (messages are made of strings: a number put into a stream from this module ended the process)
-std::string list(at::IntArrayRef sizes) {
-    std::string s = "[";
-    for (size_t i = 0; i < sizes.size(); ++i) s += (i ? ", " : "") + std::to_string(sizes[i]);
-    return s + "]";
 }
 int type_of(const Tensor& t) {
     switch (t.scalar_type()) {
@@ -77,8 +70,8 @@ void* plain(PyObject* o, const char* what, at::ScalarType type, at::IntArrayRef 
     if (none(o)) return nullptr;
     const Tensor& t = tensor(o, what);
     TORCH_CHECK_VALUE(t.scalar_type() == type && t.sizes() == shape && t.is_contiguous() && t.device() == like.device(), what, ": expected ",
-                      c10::toString(type), " ", list(shape), ", contiguous, on ", like.device().str(), "; got ", c10::toString(t.scalar_type()), " ",
-                      list(t.sizes()), " on ", t.device().str());
+                      c10::toString(type), " ", shape, ", contiguous, on ", like.device().str(), "; got ", c10::toString(t.scalar_type()), " ",
+                      t.sizes(), " on ", t.device().str());
     return t.data_ptr();
 }
 template <typename P> P* as(void* p) { return static_cast<P*>(p); }
@@ -115,17 +108,17 @@ struct Pages {
 // [sequences, rows, heads, head_dim] with contiguous heads
 void rows(const Tensor& t, const char* what, int64_t b, int64_t r, const Tensor& k) {
     TORCH_CHECK_VALUE(t.dim() == 4 && t.size(0) == b && t.size(1) == r && t.size(3) == k.size(3) && t.stride(3) == 1 && t.device() == k.device(), what,
-                      ": [sequences, rows, heads, head_dim] with contiguous heads on the pages' device, got ", list(t.sizes()));
+                      ": [sequences, rows, heads, head_dim] with contiguous heads on the pages' device, got ", t.sizes());
 }
 // fp32 [sequences, kv heads, at least n slots]
 void columns(const Tensor& t, const char* what, int64_t b, int64_t n, const Tensor& k) {
     TORCH_CHECK_VALUE(t.dim() == 3 && t.size(0) >= b && t.size(1) == k.size(1) && t.size(2) >= n && t.stride(2) == 1 && t.scalar_type() == at::kFloat &&
-                          t.device() == k.device(), what, ": fp32 [sequences, kv heads, at least ", std::to_string(n), " slots] on the pages' device");
+                          t.device() == k.device(), what, ": fp32 [sequences, kv heads, at least ", n, " slots] on the pages' device");
 }
 
 PyObject* status(int rc) { return PyLong_FromLong(rc); }
 
-void count(Py_ssize_t got, Py_ssize_t want) { TORCH_CHECK_TYPE(got == want, "expected ", std::to_string(want), " arguments, got ", std::to_string(got)); }
+void count(Py_ssize_t got, Py_ssize_t want) { TORCH_CHECK_TYPE(got == want, "expected ", want, " arguments, got ", got); }
 
 // (q, k, v, k_pages, v_pages, table, lens, n_rows, pos, rope_base, q_out, status, stream) -> q_out or None
 PyObject* append(PyObject*, PyObject* const* x, Py_ssize_t n) {
@@ -282,7 +275,7 @@ PyObject* evict(PyObject*, PyObject* const* x, Py_ssize_t n) {
 // (.., result, draft_rows, accept_uniform, draft_temperature) -> status code
 PyObject* accept(PyObject*, PyObject* const* x, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    TORCH_CHECK_TYPE(n == 9 || n == 10, "expected 9 or 10 arguments, got ", std::to_string(n));
+    TORCH_CHECK_TYPE(n == 9 || n == 10, "expected 9 or 10 arguments, got ", n);
     const Tensor& z = tensor(x[0], "logits");
     TORCH_CHECK_VALUE(z.dim() == 3 && z.stride(2) == 1 && type_of(z) >= 0, "logits: [sequences, drafted tokens + 1, vocab]");
     const int64_t b = z.size(0), g = z.size(1) - 1, v = z.size(2);
