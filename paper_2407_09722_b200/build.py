@@ -5,6 +5,7 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -26,17 +27,30 @@ def _stale(target: str, deps) -> bool:
     return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
 
 
+def _nvcc() -> str:
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    return shutil.which(nvcc) or nvcc
+
+
+def ops_stale() -> bool:
+    """Whether _ops.so is older than its sources, or was built against another torch (whose name is in it)."""
+    import torch
+    if _stale(OPS, [OPS_SRC, HEADER]):
+        return True
+    with open(OPS, "rb") as f:
+        return f"torch {torch.__version__};".encode() not in f.read()
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if force or _stale(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [HEADER]):
-        nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-        cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-t", "0",
+        cmd = [_nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-t", "0",
                "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
                "-o", LIB] + os.environ.get("MTAD_NVCC_FLAGS", "").split() + sources()
         if verbose:
             cmd.insert(1, "-Xptxas=-v")
             print(" ".join(cmd))
         subprocess.run(cmd, check=True)
-    if force or _stale(OPS, [OPS_SRC, HEADER]):
+    if force or ops_stale():
         build_ops(verbose)
     return LIB
 
@@ -44,9 +58,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
 def build_ops(verbose: bool = False) -> str:
     import torch
     t = os.path.dirname(os.path.abspath(torch.__file__))
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DMTAD_TORCH="torch {torch.__version__};"']
     for d in (os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
-              sysconfig.get_paths()["include"], "/usr/local/cuda/include"):
+              sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")):
         cmd += ["-I", d]
     # (libstdc++ by name, ahead of the compiler's own: one that comes with the archive only would put a second copy of it into the module, and
     # a number written to a stream of torch's then ends the process)

@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <optional>
+#include <string>
 
 #include "mtad.h"
 
@@ -312,8 +313,15 @@ PyMethodDef methods[] = {
     {"evict", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(evict)), METH_FASTCALL, nullptr},
     {"accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(accept)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
+// the torch that this was compiled for, "torch <version>;", as the build finds it in the file
+__attribute__((used)) const char built_for[] = MTAD_TORCH;
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__ops(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__ops(void) {
+    PyObject* m = PyModule_Create(&module);
+    const std::string name(built_for);
+    if (m && PyModule_AddStringConstant(m, "torch_version", name.substr(6, name.size() - 7).c_str()) < 0) Py_CLEAR(m);
+    return m;
+}

@@ -26,7 +26,10 @@ def _ops():
         B.load_library()
         if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_ops.so")):
             raise RuntimeError("_ops.so is missing: run `python -m paper_2407_09722_b200.build` first (there is no fallback path)")
-        _mod = importlib.import_module("._ops", __package__)
+        mod = importlib.import_module("._ops", __package__)
+        if mod.torch_version != torch.__version__:
+            raise RuntimeError(f"_ops.so was built for another torch ({mod.torch_version}): run `python -m paper_2407_09722_b200.build` again")
+        _mod = mod
     return _mod
 
 

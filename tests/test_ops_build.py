@@ -32,3 +32,25 @@ def test_messages_with_numbers():
         M.paged_attention(torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)[:, :, :, ::2], k, k, table.expand(2, -1).contiguous(), lens)
     with pytest.raises(TypeError, match="expected 14 arguments, got 2"):
         ops._ops().evict(k, k)
+
+
+def test_the_module_belongs_to_one_torch(monkeypatch):
+    """Built against another torch it is built again, and not loaded before that."""
+    from paper_2407_09722_b200 import ops
+    assert ops._ops().torch_version == torch.__version__ and not Bd.ops_stale()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "2.0.0+other")
+        assert Bd.ops_stale()
+        m.setattr(ops, "_mod", None)
+        with pytest.raises(RuntimeError, match="another torch"):
+            ops._ops()
+    assert not Bd.ops_stale()
+
+
+def test_headers_come_from_the_compiler_in_use(monkeypatch):
+    """NVCC names the toolkit, and the marshalling takes its headers from there too."""
+    seen = []
+    monkeypatch.setenv("NVCC", "/elsewhere/cuda/bin/nvcc")
+    monkeypatch.setattr(Bd.subprocess, "run", lambda cmd, **kw: seen.append(cmd))
+    Bd.build_ops()
+    assert "/elsewhere/cuda/include" in seen[0] and "/usr/local/cuda/include" not in seen[0]
