@@ -46,6 +46,12 @@ int type_of(const Tensor& t) {
 
 // (a dimension of one entry may have any stride)
 int64_t step(const Tensor& t, int d) { return t.size(d) == 1 ? 0 : t.stride(d); }
+bool alike(const Tensor& a, const Tensor& b) {
+    if (a.sizes() != b.sizes() || a.scalar_type() != b.scalar_type() || a.device() != b.device()) return false;
+    for (int d = 0; d < a.dim(); ++d)
+        if (step(a, d) != step(b, d)) return false;
+    return true;
+}
 
 // The device of a call, and its stream: what is allocated here belongs to the stream that uses it
 struct On {
@@ -83,8 +89,7 @@ struct Pages {
     int64_t slots;                   // of a table row
     Pages(PyObject* k_, PyObject* v_, PyObject* table_, int64_t batch) : k(tensor(k_, "k_pages")) {
         const Tensor &v = tensor(v_, "v_pages"), &t = tensor(table_, "table");
-        TORCH_CHECK_VALUE(k.dim() == 4 && v.sizes() == k.sizes() && v.strides() == k.strides() && v.scalar_type() == k.scalar_type() && v.device() == k.device(),
-                          "k_pages and v_pages: [pages, kv heads, slots of a page, head_dim], alike in shape, strides, type and device");
+        TORCH_CHECK_VALUE(k.dim() == 4 && alike(k, v), "k_pages and v_pages: [pages, kv heads, slots of a page, head_dim], alike in shape, strides, type and device");
         TORCH_CHECK_VALUE(t.dim() == 2 && t.scalar_type() == at::kInt && t.device() == k.device() && t.stride(1) == 1 && t.size(0) >= batch,
                           "table: int32 [sequences, pages] on the pages' device, a row for every sequence, a row contiguous");
         TORCH_CHECK_VALUE(t.size(0) <= 1 || t.stride(0) >= t.size(1), "table: rows lie apart, each of its own (of an expanded view: table.contiguous())");
@@ -129,8 +134,7 @@ PyObject* append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     const int64_t b = k.dim() == 4 ? k.size(0) : 0, r = k.dim() == 4 ? k.size(1) : 0;
     const Pages p(x[3], x[4], x[5], b);
     rows(k, "k", b, r, p.k);
-    TORCH_CHECK_VALUE(v.sizes() == k.sizes() && v.strides() == k.strides() && v.scalar_type() == k.scalar_type() && v.device() == k.device(),
-                      "v: like k in shape, strides, type and device");
+    TORCH_CHECK_VALUE(alike(k, v), "v: like k in shape, strides, type and device");
     TORCH_CHECK_VALUE(k.size(2) == p.k.size(1) && type_of(k) >= 0, "k: the pages' heads, bf16, fp16 or fp32");
     const On on(p.k, x[12]);
     mtad_paged_rows a{};

@@ -119,3 +119,20 @@ def test_as_many_sinks_as_there_are_slots_or_more(lib, sinks):
     call = dict(W, rows=40, out_stride_seq=40 * 8192, window=100, max_len=1000)
     assert lib.mtad_paged_attention_workspace(_kv(), _attn(**{**call, "window": 0}), C.byref(n)) == 0
     assert lib.mtad_paged_attention_workspace(_kv(), _attn(sinks=sinks, **call), C.byref(m)) == 0 and m.value == n.value
+
+
+def test_strides_of_single_dimensions_may_differ_between_keys_and_values():
+    """One row of one sequence, one page: whatever stands there as a stride is not stepped along (the calls end at the tensors' device)."""
+    k = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16)
+    v = k.as_strided(k.shape, (7, 9, 64, 1))
+    kp = torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16)
+    vp = kp.as_strided(kp.shape, (11, 1024, 64, 1))
+    table, lens = torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    q = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16)
+    for call in (lambda: M.paged_append(q, k, v, kp, vp, table, lens), lambda: M.paged_attention(q, kp, vp, table, lens)):
+        with pytest.raises(ValueError, match="CUDA tensors only"):
+            call()
+    with pytest.raises(ValueError, match="alike"):
+        M.paged_attention(q, kp, kp.transpose(1, 2).contiguous().transpose(1, 2), table, lens)
+    with pytest.raises(ValueError, match="like k"):
+        M.paged_append(q, k, torch.zeros(1, 1, 2, 72, dtype=torch.bfloat16)[..., :64], kp, kp, table, lens)
