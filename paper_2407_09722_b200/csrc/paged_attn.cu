@@ -14,8 +14,8 @@
 //    unnormalised output, all fp32) are joined by a second kernel whose launch the first one overlaps.
 //  - Short contexts (attn_kernel without LIST): a cluster of up to eight blocks has a head and joins its pieces through distributed shared
 //    memory, one launch and no workspace.
-//  - Copies are cp.async, three or four stages, page ids looked up a tile ahead; with up to 16 query rows a warp multiplies what it has
-//    copied itself and no barrier stands in between.
+//  - Copies are cp.async, page ids looked up a tile ahead.  Up to 16 query rows: three stages (four for heads of 64), a warp multiplies what
+//    it has copied itself and no barrier stands in between.  More rows: two stages (four for heads of 64) and a barrier a tile.
 // Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 93 us, 5.8 TB/s (a plain read of 8 GB
 // runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 61 us, 5.6 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
 // one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
@@ -60,7 +60,7 @@ struct AttnArgs {
     int cluster;                     // blocks of a head; 0: the list is cut evenly over the grid
     int grid;
     // workspace
-    int* plan;                       // [0] tiles of a block, [1 .. B + 1] first tile of every sequence
+    int* plan;                       // [0] tiles of a share, [1 .. B] first tile of every sequence
     float* part_o;                   // [2 * grid][rows_block][HD]
     float2* part_ml;                 // [2 * grid][rows_block] maximum (log2 domain) and sum
     float* row_lse2;                 // [B][Hkv * RB][rows_block] log2 of the sums of heads that one block saw whole, only with weights
@@ -763,7 +763,7 @@ __global__ void __launch_bounds__(NT, Tile<HD, ROWS>::BLOCKS) attn_kernel(const 
         if (blockIdx.x != 0 && first >= total) return;
         const int start = (int)first, end = min(total, start + min(per, total - start));
         if (blockIdx.x == 0 && (a.B > 32 || warp == 0)) { // for the second kernel
-            if (me == 0) { a.plan[0] = per; a.plan[a.B + 1] = total; }
+            if (me == 0) a.plan[0] = per;
             int x = base;
             for (int b = b0; b < b1; ++b) { a.plan[1 + b] = x; x += seq_of<TK>(a, b).nt * HR; }
         }
@@ -1414,7 +1414,7 @@ int make_plan(const mtad_paged_kv* kv, const mtad_paged_attn* c, AttnPlan* p) {
     p->grid = (int)(list ? std::min(heads * tiles, fill) : heads * cs);
     a.grid = p->narrow ? p->grid * (NT / 32) : p->grid;  // shares
     Carve w;
-    p->plan = w.take(list ? sizeof(int) * (a.B + 2) : 0);
+    p->plan = w.take(list ? sizeof(int) * (a.B + 1) : 0);
     p->part_o = w.take(list ? sizeof(float) * 2 * (size_t)a.grid * a.rows_block * p->HD : 0);
     p->part_ml = w.take(list ? sizeof(float2) * 2 * (size_t)a.grid * a.rows_block : 0);
     a.score_ld = a.weights ? (long long)((a.max_len + TK - 1) / TK) * TK : 0;
