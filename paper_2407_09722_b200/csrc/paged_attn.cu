@@ -41,7 +41,11 @@ constexpr int TK = 64;               // keys of a tile
 constexpr int NT = 128;              // threads of a block
 constexpr int MAX_ROWS_BLOCK = 64;   // query rows (rows x heads of the group) of a block
 constexpr int MAX_CLUSTER = 8;
-constexpr int CLUSTER_TILES = 12, CLUSTER_TILES_WIDE = 8;       // tiles of a block up to which a cluster has a head
+// Tiles of a block up to which a cluster has a head (device time of one sequence, cluster / list, heads of 128).  8 rows a KV head, 6144 slots (12
+// tiles in clusters of eight): 1 KV head 15.8 / 18.8 us, 4 16.3 / 19.1, 8 16.4 / 17.0; 8192 slots: 19.5 / 22.8, 19.9 / 22.1, 20.1 / 18.0; 16384
+// slots: 34 / 38, 35 / 24, 35 / 27.  40 rows, 32 KV heads: 4096 slots 37.6 / 40.9, 8192 67.2 / 67.7, 16384 123 / 116 (two blocks a head); few heads
+// would have the list from 1000 to 2000 slots on (4096 slots, 1 KV head 27.5 / 13.6, 8 27.8 / 20.7), which this rule does not know.
+constexpr int CLUSTER_TILES = 12, CLUSTER_TILES_WIDE = 8;
 
 struct AttnArgs {
     PagedView kv;
@@ -115,7 +119,8 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there, 
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
 }
 // What is read once leaves the L2 first (a long list: 61 us instead of 65 for the ragged batch of eight); what a short call has read may be there
-// when the next one asks for it, and rows in several blocks read it again.
+// when the next one asks for it, and rows in several blocks read it again.  (Pages that sequences share are taken as read once too: whether an id
+// comes again is not known here.)
 __device__ __forceinline__ uint64_t copy_policy(bool once) {
     uint64_t p;
     if (once) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -1466,7 +1471,8 @@ cudaError_t launch_hd(const AttnPlan& p, cudaStream_t st) {
     const cudaError_t e = launch_rows<T, HD, true>(p, st);
     if (e != cudaSuccess) return e;
     mtad_ops_count(1);
-    // (a head in many pieces: 296 of them took one warp 45 us)
+    // (a head in many pieces, four warps a row / one: 37 pieces 27.1 / 28.6 us a call, 148 pieces 16.1 / 24.5, 1184 pieces 22 / 49; with few, blocks of
+    // one row have too little to do)
     const long long heads = (long long)p.a.B * p.a.kv.Hkv * p.a.RB;
     const bool split = p.a.grid / heads >= 12;
     const int rows = std::min(p.a.R * p.a.G, p.a.rows_block), groups = split ? rows : (rows + 3) / 4, join = (int)heads * groups;
