@@ -21,7 +21,9 @@
 // one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
 // taken over from blocks not yet launched evened that out, and cost more than it gave), the second kernel (5 us), the first loads (4 us).
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as terms of the cache's type (p, and what
-// its rounding left; see Prob), so that they keep the bits of fp32; the output is rounded once.
+// its rounding left; see Prob), so that they keep the bits of fp32.  The tensor cores cut sums off where fp32 rounds them, so a tile's
+// products have accumulators of their own and are added to the output by fp32 additions: what is cut off, always towards zero, turned six times
+// as many roundings of bf16 outputs over long shares as sums that are rounded.  The output is rounded once.
 #include <cooperative_groups.h>
 #include <limits.h>
 #include <math_constants.h>
@@ -220,8 +222,8 @@ __device__ __forceinline__ void zero_mixed(const AttnArgs& a, const TileAt& t, i
 
 // Terms of the cache's type as which a probability enters the second product: three of bf16 hold the 24 bits of fp32, two of fp16 hold 22.
 // (Two of bf16 left 2^-18 of a probability out, which turned the rounding of one output in 2000.  The third takes no time where memory bounds
-// the call, up to 16 query rows a KV head; a chain of 5 on groups of 8, eight ragged sequences, takes 42.8 us instead of 37.9, four prompt
-// chunks of 256 rows at 2000 to 4000 slots 588 instead of 498.)
+// the call, up to 16 query rows a KV head; a chain of 5 on groups of 8, eight ragged sequences, takes 43 us instead of 38, four prompt
+// chunks of 256 rows at 2000 to 4000 slots 600 instead of 498.)
 //
 // The reference of a row's exponentials is raised only when a score passes it by 2^RAISE: sums and outputs stay far inside fp32's range,
 // and most tiles need neither a maximum over lanes nor a rescaling.
@@ -388,6 +390,7 @@ template <typename T, int HD, int ROWS> struct Narrow {
                 }
             }
         constexpr int STEP = HD / 16 < 8 ? HD / 16 : 8;   // columns' products in flight
+        constexpr bool FRESH = HD * N8 <= 256;            // (16 rows of 256 columns have no registers for it: 191 us -> 326 of nine rows at 3000 to 9000 slots)
 #pragma unroll
         for (int d0 = 0; d0 < HD / 16; d0 += STEP) {
             uint32_t va[STEP][4];
@@ -395,10 +398,19 @@ template <typename T, int HD, int ROWS> struct Narrow {
             for (int d = 0; d < STEP; ++d) ldsm4t(va[d], at_v ^ ((d0 + d) << 5));
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
+                float x[STEP][4];
 #pragma unroll
-                for (int k = 0; k < TERMS; ++k)
+                for (int d = 0; d < STEP; ++d)
 #pragma unroll
-                    for (int d = 0; d < STEP; ++d) mma<T>(o[d0 + d][n], va[d], p[k][n][0], p[k][n][1]);
+                    for (int e = 0; e < 4; ++e) x[d][e] = FRESH ? 0.f : o[d0 + d][n][e];
+#pragma unroll
+                for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+                    for (int d = 0; d < STEP; ++d) mma<T>(x[d], va[d], p[k][n][0], p[k][n][1]);
+#pragma unroll
+                for (int d = 0; d < STEP; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d0 + d][n][e] = FRESH ? o[d0 + d][n][e] + x[d][e] : x[d][e];
             }
         }
     }
@@ -578,31 +590,41 @@ template <typename T, int HD, int ROWS> struct Wide {
             zero_mixed<HD>(a, t, warp * 16, lane);
             __syncthreads();
         }
+        constexpr int TERMS = Prob<T>::TERMS;
+        uint32_t p[WK / 16][TERMS][4];
 #pragma unroll
-        for (int ks = 0; ks < WK / 16; ++ks) {
-            constexpr int TERMS = Prob<T>::TERMS;
-            uint32_t p[TERMS][4];
+        for (int ks = 0; ks < WK / 16; ++ks)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float u = s[2 * ks + (e >> 1)][(e & 1) * 2] * Prob<T>::SCALE, v = s[2 * ks + (e >> 1)][(e & 1) * 2 + 1] * Prob<T>::SCALE;
 #pragma unroll
                 for (int k = 0; k < TERMS; ++k) {
-                    p[k][e] = Num<T>::pack(u, v);
-                    const float2 x = Num<T>::unpack(p[k][e]);
+                    p[ks][k][e] = Num<T>::pack(u, v);
+                    const float2 x = Num<T>::unpack(p[ks][k][e]);
                     u -= x.x;
                     v -= x.y;
                 }
             }
+        constexpr int STEP = HD == 256 ? 4 : 8;           // columns' products in flight (two: a chunk of 256 rows 13 % slower)
 #pragma unroll
-            for (int n = 0; n < HD / 8; n += 2) {
-                uint32_t vb[4];
-                ldsm4t(vb, (at_v ^ (n << 4)) + ks * 16 * HD * 2);
+        for (int n = 0; n < HD / 8; n += STEP) {
+            float x[STEP][4];
 #pragma unroll
-                for (int k = 0; k < TERMS; ++k) {
-                    mma<T>(o[n], p[k], vb[0], vb[1]);
-                    mma<T>(o[n + 1], p[k], vb[2], vb[3]);
-                }
+            for (int d = 0; d < STEP; ++d) x[d][0] = x[d][1] = x[d][2] = x[d][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < WK / 16; ++ks) {
+                uint32_t vb[STEP / 2][4];
+#pragma unroll
+                for (int d = 0; d < STEP; d += 2) ldsm4t(vb[d / 2], (at_v ^ ((n + d) << 4)) + ks * 16 * HD * 2);
+#pragma unroll
+                for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+                    for (int d = 0; d < STEP; ++d) mma<T>(x[d], p[ks][k], vb[d / 2][(d & 1) * 2], vb[d / 2][(d & 1) * 2 + 1]);
             }
+#pragma unroll
+            for (int d = 0; d < STEP; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n + d][e] += x[d][e];
         }
     }
     __device__ __forceinline__ void join_warps(float2* s_part, float2* s_ml) {

@@ -61,6 +61,27 @@ def test_attention_probabilities_keep_their_bits(dtype, group, most):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("group", [1, 16, 20, 40])
+def test_attention_sums_over_long_shares_are_rounded(dtype, group):
+    """Values of 1 for 1024 slots, of -1 for the next 1024 with the same scores, sixteen times over: the output is nothing but errors.  The
+    shares of a head go up to P, the sum of 1024 probabilities, and back; rounded to the nearest in tiles of 16 slots that is 128 errors a period, each
+    within half a step of at most P 2^-23: a standard deviation of sqrt(16 * 128 / 12) 2^-23 P, of a total of 32 P; six of them are 2^-21.7.  (Pieces
+    that end inside a period, and references that rise, add 2^-26.)  Sums that are cut off at every product came to 2^-19.5."""
+    dt = DT[dtype]
+    B, hkv, n, hd = 64, 4, 32768, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.zeros(1, n, hkv, hd, dtype=dt, device="cuda") for _ in range(2))
+    half = torch.randn(n // 2048, 1, 1024, hkv, device="cuda", generator=g).to(dt)
+    k[0, :, :, 9] = half.expand(-1, 2, -1, -1).reshape(n, hkv)
+    v[0] = torch.tensor([1.0, -1.0], device="cuda").to(dt).repeat_interleave(1024).repeat(n // 2048)[:, None, None]
+    q = torch.zeros(B, 1, hkv * group, hd, dtype=dt, device="cuda")
+    q[..., 9] = 1
+    kp, vp, table = small_cache(k, v, 64, 0)
+    out = M.paged_attention(q, kp, vp, table.expand(B, -1).contiguous(), torch.full((B,), n, dtype=torch.int32, device="cuda"), scale=1.0)
+    assert float(out.double().abs().max()) <= 2.0 ** -21, math.log2(float(out.double().abs().max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("group", [1, 16, 20, 40])
 @pytest.mark.parametrize("n,most", [(700, 700), (30000, 30000)])
 def test_attention_many_slots_far_below_one(dtype, group, n, most):
     """The first slot has a score 17.5 above all others (what an attention sink looks like) and the value 0; the others' probabilities, 2^-25.2 each,
