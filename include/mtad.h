@@ -378,7 +378,8 @@ int mtad_paged_append(const mtad_paged_kv* kv, const mtad_paged_rows* call, void
  * table entry names no page is taken as zeros and flagged MTAD_ST_RANGE) and sizes the launch and the workspace.
  * Scores, sums and statistics are fp32; probabilities enter the product with the values as three bf16 or two fp16 terms (24 or 22
  * bits; in fp16 none below 2^-37 of the row's largest); the output is rounded once.  Results do not change from call to call.
- * The workspace (256-byte aligned) holds nothing between calls. */
+ * The workspace (256-byte aligned) holds nothing between calls; with weights it has 4 bytes for every query row (of a KV head: rounded up to 8,
+ * 16, 32 or a multiple of 64) and slot up to max_len. */
 typedef struct mtad_paged_attn {
     const int32_t *lens, *n_rows;       /* device [batch]; n_rows may be NULL */
     const void* q;                      /* device [batch][rows][n_q_heads][head_dim], the cache's type, 16-byte aligned */

@@ -16,9 +16,9 @@
 //    memory, one launch and no workspace.
 //  - Copies are cp.async, page ids looked up a tile ahead.  Up to 16 query rows: three stages (four for heads of 64), a warp multiplies what
 //    it has copied itself and no barrier stands in between.  More rows: two stages (four for heads of 64) and a barrier a tile.
-// Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 93 us, 5.8 TB/s (a plain read of 8 GB
+// Measured (device time, B200): 32 contexts behind a window of 4096, 64 heads on 8 of 128, 538 MB: 96 us, 5.6 TB/s (a plain read of 8 GB
 // runs at 6.2); eight ragged sequences x 7 rows, 40 heads, 341 MB: 61 us, 5.6 TB/s; a chain of 5 rows at 2053 slots, 32 heads: 11 us;
-// one row at 97 slots: 5.6 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
+// one row at 97 slots: 5.8 us.  What is left at the long ones: SMs that get a tenth less bandwidth than others for the same share (shares
 // taken over from blocks not yet launched evened that out, and cost more than it gave), the second kernel (5 us), the first loads (4 us).
 // Rounding: scores, statistics and sums are fp32.  Probabilities enter the second product as terms of the cache's type (p, and what
 // its rounding left; see Prob), so that they keep the bits of fp32.  The tensor cores cut sums off where fp32 rounds them, so a tile's
