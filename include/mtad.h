@@ -428,7 +428,7 @@ int mtad_paged_evict(const mtad_paged_kv* kv, const mtad_paged_eviction* call, v
  * target's row, or max(0, p - q) at a rejection (lowest id among equals; tokens with w = 0 never).  Logits of -infinity are
  * tokens of probability 0; a row that has nothing else, or a NaN or +infinity, flags MTAD_ST_NONFINITE: nothing accepted, n_out =
  * 0.  Also MTAD_ST_BAD_TOKEN, MTAD_ST_BAD_COUNT.  Outputs as for the verify calls with N = D = gamma (row_cand, row_cand_lp are not
- * written; node_LP by the first rule only). */
+ * written; node_LP by the first rule only): entries of out_tok and out_lp from n_out on are left as they were. */
 typedef struct mtad_accept_rows {
     const void* logits;                 /* device [batch][gamma + 1][vocab] */
     int64_t logits_stride_seq, logits_stride_row;             /* elements */

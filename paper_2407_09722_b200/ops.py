@@ -96,7 +96,8 @@ def _accept(where, logits, draft_tok, last_uniform, out, n_draft, temperature, s
 def accept_chain(logits: torch.Tensor, draft_tok: Optional[torch.Tensor], draft_logq: Optional[torch.Tensor], log_tau: float,
                  last_uniform: torch.Tensor, out: B.ResultBuffers, *, n_draft: Optional[torch.Tensor] = None,
                  temperature: float = 1.0, stream=None):
-    """The joint-likelihood threshold rule on the target's rows [sequences, gamma + 1, vocab]; results go to `out`."""
+    """The joint-likelihood threshold rule on the target's rows [sequences, gamma + 1, vocab]; results go to `out`
+    (of its out_tok and out_lp the first n_out entries of a sequence)."""
     _accept("mtad_accept_chain", logits, draft_tok, last_uniform, out, n_draft, temperature, stream, draft_logq, log_tau)
 
 
